@@ -24,6 +24,9 @@
  *     enqueued (argument errors) or the HIP launch failed (XATTN_ERR_HIP).
  *     xattn_last_error() gives a message for the calling thread.
  *   - Results are deterministic: the same inputs give bitwise equal outputs.
+ *   - The calls for serving after the prefill (rotary positions, paged cache, one
+ *     new token's attention, eviction) keep these conventions; their shapes
+ *     stand with them.
  *
  * Supported today: head_dim 128, block 128, stride S in {1,2,4,8,16,32,64},
  * seq a multiple of 128 and at most 262144 (NB <= 2048).
@@ -305,6 +308,150 @@ int xattn_head_error(const void *o, const void *o_ref, const xattn_dims *dims, d
  */
 int xattn_head_error_mean(const void *o, const void *o_ref, const xattn_dims *dims,
                           double *err, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Serving after the prefill: rotary positions, a paged cache of keys and
+ * values, the attention of one new token per sequence over it, and the
+ * eviction of its lightest tokens. Unlike the prefill these calls take any
+ * number of tokens (down to one) and strided inputs.
+ *
+ * Strides: `x_strides` holds 3 host int64, the distances in ELEMENTS between
+ * batch elements, heads and tokens of x[batch][heads][tokens][128]; the 128
+ * values of a vector are contiguous. Strides are >= 0 and multiples of 8 (the
+ * stride of a dimension of size 1 is not used); every array of bfloat16 or
+ * cache values is 16-byte aligned. Read during the call only.
+ */
+
+/* Rotary positions: the 64 pairs of a head are shared out among `axes` position
+ * axes (e.g. time, height, width), pairs[a] to axis a in order; the pairs
+ * behind them are not rotated.
+ *   interleaved  0: pair i is elements (i, i + 64); 1: (2 i, 2 i + 1)
+ *   freq         host double [sum of pairs]: radians per position, finite; read
+ *                during the call only (copied into the launch) */
+typedef struct xattn_rotary_plan {
+    int32_t axes;     /* 1 .. 3 */
+    int32_t pairs[3]; /* each >= 0 (>= 1 for a < axes, 0 behind), sum <= 64 */
+    int32_t interleaved;
+    const double *freq;
+} xattn_rotary_plan;
+
+/*
+ * Rotates every pair (x, y) of every vector by phi = pos * freq:
+ * (x cos phi - y sin phi, x sin phi + y cos phi), or by -phi if `inverse`
+ * (the inverse rotation, its transpose and therefore its gradient).
+ *   x    bf16 [batch][heads][tokens][128], strided   (e.g. a projection's output
+ *        [batch][tokens][heads][128])
+ *   pos  int32 [axes][batch][tokens] device, any values
+ *   out  bf16, same shape, strided; x itself with x's strides, or no memory of x
+ * Angles are products in fp64, reduced to a turn before they are rounded, so
+ * far positions are as exact as near ones; the rotation is fp32, rounded once.
+ * XATTN_ERR_ARG for a bad plan, stride, alignment or NULL.
+ */
+int xattn_rotary(const void *x, const int64_t *x_strides, int batch, int heads, int tokens,
+                 int head_dim, const int32_t *pos, const xattn_rotary_plan *plan, int inverse,
+                 void *out, const int64_t *out_strides, void *stream);
+
+/* A pool of pages that hold the keys and values of `page` tokens each:
+ *   k, v              [pages][hkv][page][128], bf16 or OCP e4m3 (device)
+ *   k_scale, v_scale  uint8 [pages][hkv][page] (device; e4m3 only, else NULL):
+ *                     a vector's values are its e4m3 values times
+ *                     2^(byte - 127), byte 1 .. 254
+ * A sequence's pages are a row of a page table int32 [batch][table_pages]
+ * (device): token t is row t % page of page table[b][t / page]. Entries outside
+ * 0 .. pages-1 stand for no page: what they would hold is neither read nor
+ * written (its keys are not attended to). Sequences may share pages. */
+enum xattn_cache_type { XATTN_CACHE_BF16 = 0, XATTN_CACHE_E4M3 = 1 };
+typedef struct xattn_cache {
+    int32_t pages;
+    int32_t page; /* 16, 32, 64, 128 or 256 */
+    int32_t hkv;
+    int32_t head_dim; /* 128 */
+    int32_t type;
+    void *k;
+    void *v;
+    uint8_t *k_scale;
+    uint8_t *v_scale;
+} xattn_cache;
+
+/*
+ * Writes new tokens into their pages: token t < count[b] of sequence b becomes
+ * token start[b] + t of its page table's row, its key rotated on the way if a
+ * plan is given. Nothing else is written; tokens whose place is negative or
+ * behind the table's row are not stored.
+ *   k, v    bf16 [batch][hkv][tokens][128], strided
+ *   start   int32 [batch] device
+ *   count   int32 [batch] device, or NULL for `tokens` everywhere (larger values
+ *           count as `tokens`, negative ones as 0)
+ *   pos     int32 [axes][batch][tokens] device, with plan; both NULL: no rotation
+ * bf16: a rotated key is rounded once, all else copied. e4m3: the scale is the
+ * least power of two (at least 2^-126) that brings the vector's largest finite
+ * magnitude to at most 448 (1 for a vector of zeros); a key that is rotated
+ * takes the largest length of a pair instead, which bounds it whatever the angle
+ * (a pair of which one value is not finite counts with the other). Values are
+ * rounded to nearest even; infinities become +-448, NaN stays NaN.
+ * No place may be written twice in a call (a page in two tables' rows, for
+ * instance): which of the tokens it then holds is not defined.
+ */
+int xattn_cache_append(const void *k, const int64_t *k_strides, const void *v,
+                       const int64_t *v_strides, int batch, int tokens, const int32_t *count,
+                       const int32_t *start, const int32_t *table, int table_pages,
+                       const int32_t *pos, const xattn_rotary_plan *plan,
+                       const xattn_cache *cache, void *stream);
+
+/*
+ * Attention of one new token per sequence over its cached tokens
+ * t < lens[b] (clamped to 0 .. table_pages * page):
+ *   o[b][h]   = sum_t softmax_t(q[b][h] . k_t / sqrt(128)) v_t
+ *   lse[b][h] = log sum_t exp(q[b][h] . k_t / sqrt(128))      (natural log)
+ * with the head's keys and values (contiguous GQA grouping, any group size).
+ * The new token's own key is one of the cached ones: append first. Rows without
+ * a key get o = 0 and lse = -inf; keys whose products are -inf have no weight.
+ * Several new tokens of one sequence are several rows with the same pages and
+ * each its own length.
+ *   q        bf16 [batch][hq][128]; o the same (output)
+ *   lens     int32 [batch] device
+ *   lse      fp32 [batch][hq] (output) or NULL
+ *   weights  fp32 [batch][hkv][table_pages * page] (updated) or NULL: entry t of
+ *            a key head grows by the sum of its query heads' softmax_t, for
+ *            t < lens[b]; what lies behind is left as it was
+ *   workspace  at least xattn_decode_workspace_size() bytes (`weights`: whether
+ *            the call has them); its contents on entry are ignored
+ * QK^T is bf16 on the matrix cores (e4m3 keys are exact in bf16) with fp32
+ * accumulation; the softmax, P and the PV product are fp32, the output rounded
+ * once.
+ */
+int xattn_decode_workspace_size(const xattn_cache *cache, int batch, int hq, int table_pages,
+                                int weights, size_t *bytes);
+int xattn_decode(const void *q, const xattn_cache *cache, int batch, int hq,
+                 const int32_t *table, int table_pages, const int32_t *lens, void *o, float *lse,
+                 float *weights, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Eviction by accumulated attention weight: of each sequence and key head the
+ * `budget` tokens that are worth most move, in their order, to the pages of
+ * another table. Sequences of at most `budget` tokens move whole. Of longer
+ * ones the last `recent` tokens stay, and of those before them the
+ * budget - recent of the largest weight (equal weights: the earlier token; NaN
+ * is below every number). Each key head keeps its own tokens: keys carry their
+ * positions, the heads need not agree. The old pages are only read, so they may
+ * be shared with other sequences; free them afterwards.
+ *   table, lens  the sequences before: int32 [batch][table_pages], [batch];
+ *                lens clamped to 0 .. table_pages * page
+ *   weights      fp32 [batch][hkv][table_pages * page] (e.g. from xattn_decode)
+ *   new_table    int32 [batch][new_pages]: distinct pages, none of them in
+ *                `table`; new_pages * page >= budget
+ *   kept         int32 [batch][hkv][budget] (output): the tokens kept, ascending,
+ *                -1 behind them
+ *   new_lens     int32 [batch] (output): min(lens, budget); must not be lens
+ *   new_weights  fp32 [batch][hkv][new_pages * page] (output): the kept tokens'
+ *                weights, 0 behind them; no memory of weights
+ * 1 <= budget, 0 <= recent <= budget. Page rows behind the kept tokens are left
+ * as they were.
+ */
+int xattn_cache_evict(const xattn_cache *cache, int batch, const int32_t *table, int table_pages,
+                      const int32_t *lens, const float *weights, int budget, int recent,
+                      const int32_t *new_table, int new_pages, int32_t *kept, int32_t *new_lens,
+                      float *new_weights, void *stream);
 
 /* Static description of a status code (never NULL). */
 const char *xattn_strerror(int status);

@@ -56,6 +56,18 @@ class Dims(ctypes.Structure):
         return self.batch * self.hq
 
 
+class RotaryPlan(ctypes.Structure):
+    _fields_ = [("axes", ctypes.c_int32), ("pairs", ctypes.c_int32 * 3),
+                ("interleaved", ctypes.c_int32), ("freq", ctypes.c_void_p)]
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_int32), ("page", ctypes.c_int32), ("hkv", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("type", ctypes.c_int32), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p)]
+
+
 EXPORTS = [
     "xattn_score_workspace_size", "xattn_score", "xattn_score_pattern", "xattn_select",
     "xattn_select_heads",
@@ -64,6 +76,8 @@ EXPORTS = [
     "xattn_forward", "xattn_forward_noalloc", "xattn_forward_scheduled", "xattn_threshold_dp",
     "xattn_threshold_levels", "xattn_threshold_predict",
     "xattn_head_error_workspace_size", "xattn_head_error", "xattn_head_error_mean",
+    "xattn_rotary", "xattn_cache_append", "xattn_decode_workspace_size", "xattn_decode",
+    "xattn_cache_evict",
     "xattn_strerror", "xattn_last_error", "xattn_version",
 ]
 
@@ -102,6 +116,12 @@ def lib() -> ctypes.CDLL:
         L.xattn_head_error_workspace_size.argtypes = [PD, PSZ]
         L.xattn_head_error.argtypes = [P, P, PD, P, P, SZ, P]
         L.xattn_head_error_mean.argtypes = [P, P, PD, P, P, SZ, P]
+        PP, PC = ctypes.POINTER(RotaryPlan), ctypes.POINTER(Cache)
+        L.xattn_rotary.argtypes = [P, P, I, I, I, I, P, PP, I, P, P, P]
+        L.xattn_cache_append.argtypes = [P, P, P, P, I, I, P, P, P, I, P, PP, PC, P]
+        L.xattn_decode_workspace_size.argtypes = [PC, I, I, I, I, PSZ]
+        L.xattn_decode.argtypes = [P, PC, I, I, P, I, P, P, P, P, P, SZ, P]
+        L.xattn_cache_evict.argtypes = [PC, I, P, I, P, P, I, I, P, I, P, P, P, P]
         L.xattn_strerror.argtypes = [I]
         L.xattn_strerror.restype = ctypes.c_char_p
         L.xattn_last_error.restype = ctypes.c_char_p

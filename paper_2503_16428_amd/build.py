@@ -20,7 +20,8 @@ OUT_DIR = os.path.join(HERE, "lib")
 LIB = os.path.join(OUT_DIR, "libxattn.so")
 PROBE_LIB = os.path.join(OUT_DIR, "libxattn_probe.so")
 C_CLIENT = os.path.join(OUT_DIR, "xattn_c_client")
-SOURCES = ["score.hip", "select.hip", "attn.hip", "error.hip", "noalloc.hip", "api.cpp",
+SOURCES = ["score.hip", "select.hip", "attn.hip", "error.hip", "noalloc.hip", "rotary.hip",
+           "decode.hip", "evict.hip", "api.cpp", "serve.cpp",
            "threshold.cpp"]
 PROBE_SOURCES = ["probe.hip"]
 ARCH = "gfx950"

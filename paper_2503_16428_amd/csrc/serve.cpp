@@ -1,0 +1,255 @@
+// C ABI of the calls for serving after the prefill: argument validation and
+// workspace sizing. Declarations and contracts are in include/xattn.h.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "serve.h"
+#include "xattn.h"
+
+namespace xattn_host {
+extern thread_local char g_err[512];
+int fail(int code, const char* fmt, ...);
+}  // namespace xattn_host
+
+namespace {
+
+using xattn_host::fail;
+using xattn::CacheParams;
+using xattn::RotaryParams;
+using xattn::Strides;
+
+int ok() {
+  xattn_host::g_err[0] = '\0';
+  return XATTN_OK;
+}
+
+int launched(hipError_t e, const char* what) {
+  if (e != hipSuccess) return fail(XATTN_ERR_HIP, "%s launch: %s", what, hipGetErrorString(e));
+  return ok();
+}
+
+int check_pointer(const void* p, const char* name, size_t align) {
+  if (!p) return fail(XATTN_ERR_ARG, "%s must be non-NULL", name);
+  if ((uintptr_t)p % align != 0)
+    return fail(XATTN_ERR_ARG, "%s must be aligned to %zu bytes", name, align);
+  return XATTN_OK;
+}
+
+// Strides of [batch][heads][tokens] vectors; of a dimension of size 1 unused.
+int check_strides(const int64_t* s, const char* name, int batch, int heads, int tokens,
+                  bool written, Strides* out) {
+  if (!s) return fail(XATTN_ERR_ARG, "the strides of %s are NULL", name);
+  const int size[3] = {batch, heads, tokens};
+  long long v[3];
+  for (int i = 0; i < 3; ++i) {
+    v[i] = size[i] == 1 ? 0 : s[i];
+    if (v[i] < 0 || v[i] % 8 != 0 || v[i] > (1ll << 40))
+      return fail(XATTN_ERR_ARG, "stride %d of %s must be a multiple of 8 from 0 to 2^40 (got %lld)",
+                  i, name, (long long)s[i]);
+    if (written && size[i] > 1 && v[i] < xattn::kHeadDim)
+      return fail(XATTN_ERR_ARG, "stride %d of the output %s lets its vectors overlap (%lld)", i,
+                  name, (long long)s[i]);
+  }
+  *out = Strides{v[0], v[1], v[2]};
+  return XATTN_OK;
+}
+
+constexpr double kTwoPi = 6.283185307179586476925286766559;
+
+int check_plan(const xattn_rotary_plan* plan, RotaryParams* out) {
+  if (!plan) return fail(XATTN_ERR_ARG, "plan is NULL");
+  if (plan->axes < 1 || plan->axes > 3)
+    return fail(XATTN_ERR_ARG, "axes must be 1, 2 or 3 (got %d)", plan->axes);
+  if (plan->interleaved != 0 && plan->interleaved != 1)
+    return fail(XATTN_ERR_ARG, "interleaved must be 0 or 1 (got %d)", plan->interleaved);
+  if (!plan->freq) return fail(XATTN_ERR_ARG, "freq is NULL");
+  *out = RotaryParams{};
+  int n = 0;
+  for (int a = 0; a < 3; ++a) {
+    const int pairs = plan->pairs[a];
+    if (a < plan->axes ? pairs < 1 || pairs > 64 : pairs != 0)
+      return fail(XATTN_ERR_ARG, "pairs[%d] = %d with %d axes", a, pairs, plan->axes);
+    if (n + pairs > 64) return fail(XATTN_ERR_ARG, "more than 64 pairs");
+    for (int i = 0; i < pairs; ++i, ++n) {
+      if (!std::isfinite(plan->freq[n])) return fail(XATTN_ERR_ARG, "freq[%d] is not finite", n);
+      out->turn[n] = plan->freq[n] / kTwoPi;
+      out->axis[n] = (unsigned char)a;
+    }
+  }
+  out->n = n;
+  return XATTN_OK;
+}
+
+int check_tokens(int batch, int heads, int tokens) {
+  if (batch < 1 || heads < 1 || tokens < 1)
+    return fail(XATTN_ERR_ARG, "sizes must be positive (batch=%d heads=%d tokens=%d)", batch, heads,
+                tokens);
+  if ((long long)batch * tokens > (1ll << 28) || heads > 65535)
+    return fail(XATTN_ERR_UNSUPPORTED, "more than 2^28 tokens or 65535 heads");
+  return XATTN_OK;
+}
+
+int check_cache(const xattn_cache* cache, const int32_t* table, int table_pages, int batch,
+                CacheParams* out) {
+  if (!cache) return fail(XATTN_ERR_ARG, "cache is NULL");
+  int shift = 4;
+  while (shift < 8 && cache->page != 1 << shift) ++shift;
+  if (cache->page != 1 << shift)
+    return fail(XATTN_ERR_ARG, "page must be 16, 32, 64, 128 or 256 (got %d)", cache->page);
+  if (cache->pages < 1 || cache->hkv < 1 || cache->head_dim < 1)
+    return fail(XATTN_ERR_ARG, "pages, hkv and head_dim must be positive (%d, %d, %d)",
+                cache->pages, cache->hkv, cache->head_dim);
+  if (cache->head_dim != xattn::kHeadDim)
+    return fail(XATTN_ERR_UNSUPPORTED, "head_dim %d not supported (only %d)", cache->head_dim,
+                xattn::kHeadDim);
+  if (cache->type != XATTN_CACHE_BF16 && cache->type != XATTN_CACHE_E4M3)
+    return fail(XATTN_ERR_ARG, "unknown cache type %d", cache->type);
+  if (batch < 1) return fail(XATTN_ERR_ARG, "batch must be positive (got %d)", batch);
+  if (table_pages < 1)
+    return fail(XATTN_ERR_ARG, "the page table must have columns (got %d)", table_pages);
+  if ((long long)table_pages << shift > (1ll << 30))
+    return fail(XATTN_ERR_UNSUPPORTED, "a page table row of more than 2^30 tokens");
+  if ((long long)batch * cache->hkv > 65535 * 16ll)
+    return fail(XATTN_ERR_UNSUPPORTED, "more than 2^20 sequences times key heads");
+  *out = CacheParams{cache->k, cache->v, cache->k_scale, cache->v_scale, table, cache->pages,
+                     shift, cache->hkv, table_pages};
+  return XATTN_OK;
+}
+
+int check_cache_arrays(const xattn_cache* c, const int32_t* table) {
+  int rc;
+  if ((rc = check_pointer(c->k, "the cache's k", 16)) ||
+      (rc = check_pointer(c->v, "the cache's v", 16)) ||
+      (rc = check_pointer(table, "table", 4)))
+    return rc;
+  if (c->type == XATTN_CACHE_E4M3)
+    if ((rc = check_pointer(c->k_scale, "the cache's k_scale", 4)) ||
+        (rc = check_pointer(c->v_scale, "the cache's v_scale", 4)))
+      return rc;
+  return XATTN_OK;
+}
+
+int check_decode(const xattn_cache* cache, int batch, int hq, const int32_t* table,
+                 int table_pages, CacheParams* c) {
+  int rc;
+  if ((rc = check_cache(cache, table, table_pages, batch, c))) return rc;
+  if (hq < 1 || hq % cache->hkv != 0)
+    return fail(XATTN_ERR_ARG, "hq (%d) must be a positive multiple of hkv (%d)", hq, cache->hkv);
+  // grids of one workgroup a head, and of one a head and 256 tokens
+  if ((long long)batch * hq > (1 << 20) ||
+      (long long)batch * cache->hkv * ((c->capacity() + 255) / 256) > (1 << 23))
+    return fail(XATTN_ERR_UNSUPPORTED, "more than 2^20 query heads or 2^31 cached vectors a batch");
+  return XATTN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int xattn_rotary(const void* x, const int64_t* x_strides, int batch, int heads, int tokens,
+                 int head_dim, const int32_t* pos, const xattn_rotary_plan* plan, int inverse,
+                 void* out, const int64_t* out_strides, void* stream) {
+  int rc;
+  Strides xs, os;
+  RotaryParams p;
+  if ((rc = check_tokens(batch, heads, tokens))) return rc;
+  if (head_dim != xattn::kHeadDim)
+    return fail(head_dim < 1 ? XATTN_ERR_ARG : XATTN_ERR_UNSUPPORTED,
+                "head_dim %d not supported (only %d)", head_dim, xattn::kHeadDim);
+  if (inverse != 0 && inverse != 1)
+    return fail(XATTN_ERR_ARG, "inverse must be 0 or 1 (got %d)", inverse);
+  if ((rc = check_plan(plan, &p)) ||
+      (rc = check_strides(x_strides, "x", batch, heads, tokens, false, &xs)) ||
+      (rc = check_strides(out_strides, "out", batch, heads, tokens, true, &os)) ||
+      (rc = check_pointer(x, "x", 16)) || (rc = check_pointer(out, "out", 16)) ||
+      (rc = check_pointer(pos, "pos", 4)))
+    return rc;
+  return launched(launch_rotary(x, xs, batch, heads, tokens, pos, p, plan->interleaved != 0,
+                                inverse != 0, out, os, (hipStream_t)stream),
+                  "xattn_rotary");
+}
+
+int xattn_cache_append(const void* k, const int64_t* k_strides, const void* v,
+                       const int64_t* v_strides, int batch, int tokens, const int32_t* count,
+                       const int32_t* start, const int32_t* table, int table_pages,
+                       const int32_t* pos, const xattn_rotary_plan* plan,
+                       const xattn_cache* cache, void* stream) {
+  int rc;
+  CacheParams c;
+  Strides ks, vs;
+  RotaryParams p;
+  if ((rc = check_cache(cache, table, table_pages, batch, &c)) ||
+      (rc = check_tokens(batch, cache->hkv, tokens)))
+    return rc;
+  if (!pos != !plan) return fail(XATTN_ERR_ARG, "pos and plan go together");
+  if ((plan && (rc = check_plan(plan, &p))) ||
+      (rc = check_strides(k_strides, "k", batch, cache->hkv, tokens, false, &ks)) ||
+      (rc = check_strides(v_strides, "v", batch, cache->hkv, tokens, false, &vs)) ||
+      (rc = check_pointer(k, "k", 16)) || (rc = check_pointer(v, "v", 16)) ||
+      (rc = check_pointer(start, "start", 4)) || (rc = check_cache_arrays(cache, table)))
+    return rc;
+  return launched(launch_append(k, ks, v, vs, batch, tokens, count, start, pos,
+                                plan ? &p : nullptr, plan && plan->interleaved, c,
+                                cache->type == XATTN_CACHE_E4M3, (hipStream_t)stream),
+                  "xattn_cache_append");
+}
+
+int xattn_decode_workspace_size(const xattn_cache* cache, int batch, int hq, int table_pages,
+                                int weights, size_t* bytes) {
+  int rc;
+  CacheParams c;
+  if ((rc = check_decode(cache, batch, hq, nullptr, table_pages, &c))) return rc;
+  if (!bytes) return fail(XATTN_ERR_ARG, "bytes is NULL");
+  *bytes = decode_scratch_bytes(c, batch, hq, weights != 0);
+  return ok();
+}
+
+int xattn_decode(const void* q, const xattn_cache* cache, int batch, int hq,
+                 const int32_t* table, int table_pages, const int32_t* lens, void* o, float* lse,
+                 float* weights, void* workspace, size_t workspace_bytes, void* stream) {
+  int rc;
+  CacheParams c;
+  if ((rc = check_decode(cache, batch, hq, table, table_pages, &c)) ||
+      (rc = check_pointer(q, "q", 16)) || (rc = check_pointer(o, "o", 16)) ||
+      (rc = check_pointer(lens, "lens", 4)) || (rc = check_cache_arrays(cache, table)))
+    return rc;
+  const size_t need = decode_scratch_bytes(c, batch, hq, weights != nullptr);
+  if (!workspace || workspace_bytes < need || (uintptr_t)workspace % 16 != 0)
+    return fail(XATTN_ERR_WORKSPACE, "a 16-byte aligned workspace of %zu bytes needed, %zu given",
+                need, workspace ? workspace_bytes : (size_t)0);
+  return launched(launch_decode(q, c, cache->type == XATTN_CACHE_E4M3, batch, hq, lens, o, lse,
+                                weights, workspace, (hipStream_t)stream),
+                  "xattn_decode");
+}
+
+int xattn_cache_evict(const xattn_cache* cache, int batch, const int32_t* table, int table_pages,
+                      const int32_t* lens, const float* weights, int budget, int recent,
+                      const int32_t* new_table, int new_pages, int32_t* kept, int32_t* new_lens,
+                      float* new_weights, void* stream) {
+  int rc;
+  CacheParams c;
+  if ((rc = check_cache(cache, table, table_pages, batch, &c))) return rc;
+  if (budget < 1 || recent < 0 || recent > budget)
+    return fail(XATTN_ERR_ARG, "1 <= budget and 0 <= recent <= budget (got %d, %d)", budget,
+                recent);
+  if (new_pages < 1 || ((long long)new_pages << c.shift) < budget)
+    return fail(XATTN_ERR_ARG, "%d new pages do not hold a budget of %d", new_pages, budget);
+  if ((long long)new_pages << c.shift > (1ll << 30) ||
+      (long long)batch * c.hkv * ((budget + 15) / 16) > (1 << 23))
+    return fail(XATTN_ERR_UNSUPPORTED, "more than 2^27 kept vectors a batch");
+  if ((rc = check_cache_arrays(cache, table)) || (rc = check_pointer(lens, "lens", 4)) ||
+      (rc = check_pointer(weights, "weights", 4)) ||
+      (rc = check_pointer(new_table, "new_table", 4)) || (rc = check_pointer(kept, "kept", 4)) ||
+      (rc = check_pointer(new_lens, "new_lens", 4)) ||
+      (rc = check_pointer(new_weights, "new_weights", 4)))
+    return rc;
+  if (new_lens == lens || new_weights == weights || new_table == table)
+    return fail(XATTN_ERR_ARG, "an output is its own input, or new_table is table");
+  return launched(launch_evict(c, cache->type == XATTN_CACHE_E4M3, batch, lens, weights, budget,
+                               recent, new_table, new_pages, kept, new_lens, new_weights,
+                               (hipStream_t)stream),
+                  "xattn_cache_evict");
+}
+
+}  // extern "C"

@@ -1,0 +1,328 @@
+"""Binding of the calls for serving after the prefill: rotary positions, the
+paged cache, one new token's attention and eviction (include/xattn.h).
+
+Argument checks and marshalling only, as in binding.py; every tensor is on the
+current device.
+
+Tensor layouts:
+  vectors  bf16 [batch, heads, tokens, 128] or [heads, tokens, 128], any strides
+           that keep a vector's 128 values together and 16-byte aligned
+  cache    bf16 or float8_e4m3fn [pages, hkv, page, 128] (KVCache)
+  table    int32 [batch, table_pages]; -1 (any value outside 0 .. pages-1): no page
+  weights  fp32 [batch, hkv, table_pages * page]
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes
+
+import numpy as np
+import torch
+
+from .binding import (XATTN_ERR_ARG, Cache, RotaryPlan, XAttnError, _check, _check_shape,
+                      _check_workspace, _need, _ptr, lib)
+
+HEAD_DIM = 128
+_PAGES = (16, 32, 64, 128, 256)
+_I3 = ctypes.c_int64 * 3
+
+
+def _fail(message):
+    raise XAttnError(XATTN_ERR_ARG, message)
+
+
+def rotary_freqs(pairs, base: float = 10000.0, restart: bool = False) -> np.ndarray:
+    """The usual frequencies of Rotary: pair i of n rotates by base^(-i/n) a position, counted
+    over all axes, or from 0 for each axis of `pairs` (restart)."""
+    if restart:
+        return np.concatenate([float(base) ** (-np.arange(n) / n) for n in pairs])
+    n = int(sum(pairs))
+    return float(base) ** (-np.arange(n) / n)
+
+
+class Rotary:
+    """Rotary positions of one model: pairs[a] of a head's 64 pairs turn with position axis a, by
+    freq (float64, one a pair, radians per position); pair i is elements (2i, 2i+1) if interleaved,
+    else (i, i+64). Pairs behind them are not rotated."""
+
+    def __init__(self, pairs, freq, interleaved: bool = False):
+        pairs = [int(n) for n in pairs]
+        if not 1 <= len(pairs) <= 3 or min(pairs) < 1 or sum(pairs) > 64:
+            _fail(f"pairs must be 1 to 3 positive numbers of sum <= 64, got {pairs}")
+        self._freq = np.array(freq, dtype=np.float64)  # a copy: the plan points into it
+        if self._freq.shape != (sum(pairs),) or not np.isfinite(self._freq).all():
+            _fail(f"freq must be {sum(pairs)} finite numbers")
+        self.pairs, self.interleaved = tuple(pairs), bool(interleaved)
+        self._plan = RotaryPlan(len(pairs), (ctypes.c_int32 * 3)(*pairs), int(self.interleaved),
+                                self._freq.ctypes.data)
+        self._ref = ctypes.byref(self._plan)
+
+    @property
+    def axes(self) -> int:
+        return len(self.pairs)
+
+
+class KVCache:
+    """A pool of pages: k, v [pages, hkv, page, 128], bf16, or float8_e4m3fn with the bytes of
+    their power-of-two scales k_scale, v_scale uint8 [pages, hkv, page]."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        if k.dim() != 4 or k.shape[3] != HEAD_DIM or k.shape[2] not in _PAGES or 0 in k.shape:
+            _fail(f"k must be [pages, hkv, page, {HEAD_DIM}] with pages of {_PAGES} tokens, got "
+                  f"{tuple(k.shape)}")
+        if k.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+            _fail(f"k must be torch.bfloat16 or torch.float8_e4m3fn, got {k.dtype}")
+        _check_shape(v, k.shape, k.dtype, "v")
+        self.e4m3 = k.dtype != torch.bfloat16
+        if self.e4m3:
+            if k_scale is None or v_scale is None:
+                _fail("an e4m3 cache needs k_scale and v_scale")
+            for t, n in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+                _check_shape(t, k.shape[:3], torch.uint8, n)
+        elif k_scale is not None or v_scale is not None:
+            _fail("a bf16 cache has no scales")
+        arrays = [t for t in (k, v, k_scale, v_scale) if t is not None]
+        for t, n in zip(arrays, ("k", "v", "k_scale", "v_scale")):
+            _need(t, t.dtype, n)
+            if t.device != k.device:
+                _fail(f"{n} must be on k's device {k.device}, got {t.device}")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.pages, self.hkv, self.page = (int(n) for n in k.shape[:3])
+        self.device = k.device
+        self._struct = Cache(self.pages, self.page, self.hkv, HEAD_DIM, int(self.e4m3), _ptr(k),
+                             _ptr(v), _ptr(k_scale), _ptr(v_scale))
+        self._ref = ctypes.byref(self._struct)
+
+    @classmethod
+    def empty(cls, pages, hkv, page=64, dtype=torch.bfloat16, device="cuda"):
+        """A pool of zeros."""
+        def zeros(*shape, dtype):
+            return torch.zeros(shape, dtype=dtype, device=device)
+        if dtype == torch.bfloat16:
+            return cls(*[zeros(pages, hkv, page, HEAD_DIM, dtype=dtype) for _ in "kv"])
+        if dtype != torch.float8_e4m3fn:
+            _fail(f"dtype must be torch.bfloat16 or torch.float8_e4m3fn, got {dtype}")
+        kv = [zeros(pages, hkv, page, HEAD_DIM, dtype=torch.uint8).view(dtype) for _ in "kv"]
+        return cls(*kv, *[zeros(pages, hkv, page, dtype=torch.uint8).fill_(127) for _ in "kv"])
+
+
+def _here(**tensors):
+    """Every tensor contiguous and on the current device, where the stream is."""
+    at = None
+    for n, t in tensors.items():
+        if t is None:
+            continue
+        if not t.is_cuda:
+            _fail(f"{n} must be a device tensor")
+        if not t.is_contiguous():
+            _fail(f"{n} must be contiguous")
+        if at is None:
+            at = torch.cuda.current_device()
+        if t.get_device() != at:
+            _fail(f"{n} must be on the current device {at}, got {t.device}")
+
+
+def _vectors(t, name, like=None):
+    """(batch, heads, tokens, strides) of bf16 vectors, checked but for the device."""
+    if t.dtype != torch.bfloat16:
+        _fail(f"{name} must be torch.bfloat16, got {t.dtype}")
+    shape, strides = tuple(t.shape), t.stride()
+    if len(shape) == 3:
+        shape, strides = (1, *shape), (0, *strides)
+    if len(shape) != 4 or shape[3] != HEAD_DIM or 0 in shape:
+        _fail(f"{name} must be [batch, heads, tokens, {HEAD_DIM}] or [heads, tokens, {HEAD_DIM}], "
+              f"got {tuple(t.shape)}")
+    if like is not None and tuple(t.shape) != tuple(like.shape):
+        _fail(f"{name} must have shape {tuple(like.shape)}, got {tuple(t.shape)}")
+    if strides[3] != 1:
+        _fail(f"the {HEAD_DIM} values of a vector of {name} must be contiguous")
+    return shape[0], shape[1], shape[2], _I3(*strides[:3])
+
+
+def _on_vectors_device(**tensors):
+    at = None
+    for n, t in tensors.items():
+        if not t.is_cuda:
+            _fail(f"{n} must be a device tensor")
+        if at is None:
+            at = torch.cuda.current_device()
+        if t.get_device() != at:
+            _fail(f"{n} must be on the current device {at}, got {t.device}")
+
+
+def _positions(pos, rotary, batch, tokens, dims):
+    if not isinstance(rotary, Rotary):
+        _fail(f"rotary must be a Rotary, got {type(rotary).__name__}")
+    shape = (rotary.axes, batch, tokens) if dims == 4 else (rotary.axes, tokens)
+    _check_shape(pos, shape, torch.int32, "pos")
+
+
+def _is_cache(cache):
+    if not isinstance(cache, KVCache):
+        _fail(f"cache must be a KVCache, got {type(cache).__name__}")
+
+
+def _table(table, batch, name="table"):
+    if table.dim() != 2 or table.shape[0] != batch or table.shape[1] < 1:
+        _fail(f"{name} must be [{batch}, pages], got {tuple(table.shape)}")
+    if table.dtype != torch.int32:
+        _fail(f"{name} must be torch.int32, got {table.dtype}")
+
+
+def _extent(t):
+    """First and last byte of a strided tensor."""
+    last = sum((n - 1) * s for n, s in zip(t.shape, t.stride()))
+    return t.data_ptr(), t.data_ptr() + (last + 1) * t.element_size()
+
+
+def _apart(a, b):
+    (a0, a1), (b0, b1) = _extent(a), _extent(b)
+    return a1 <= b0 or b1 <= a0
+
+
+@contextlib.contextmanager
+def _nothing():
+    yield
+
+
+def _allocating(stream):
+    """What a call allocates belongs to the stream that it runs on."""
+    return _nothing() if stream is None else torch.cuda.stream(stream)
+
+
+def _handle(stream):
+    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+
+
+def xattn_rotary(x, pos, rotary: Rotary, inverse=False, out=None, stream=None):
+    """x rotated by its positions (back with inverse, which is also the gradient). pos int32
+    [axes, batch, tokens] ([axes, tokens] for 3-D x). out: contiguous if not given; may be x."""
+    b, h, n, xs = _vectors(x, "x")
+    _positions(pos, rotary, b, n, x.dim())
+    if out is not None:
+        _, _, _, os = _vectors(out, "out", x)
+        _on_vectors_device(x=x, out=out)
+        if not (out.data_ptr() == x.data_ptr() and out.stride() == x.stride()) \
+                and not _apart(out, x):
+            _fail("out must be x itself or lie apart from it")
+    _on_vectors_device(x=x, pos=pos)
+    if not pos.is_contiguous():
+        _fail("pos must be contiguous")
+    if out is None:
+        with _allocating(stream):
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        os = _I3(h * n * HEAD_DIM, n * HEAD_DIM, HEAD_DIM)
+    _check(lib().xattn_rotary(_ptr(x), xs, b, h, n, HEAD_DIM, _ptr(pos), rotary._ref,
+                              int(bool(inverse)), _ptr(out), os, _handle(stream)))
+    return out
+
+
+def xattn_cache_append(k, v, cache: KVCache, table, start, count=None, pos=None, rotary=None,
+                       stream=None):
+    """Writes k, v [batch, hkv, tokens, 128] as tokens start[b] .. of each sequence (count[b] of
+    them, or all) into the cache's pages, the keys rotated by pos if rotary is given."""
+    _is_cache(cache)
+    b, h, n, ks = _vectors(k, "k")
+    _, _, _, vs = _vectors(v, "v", k)
+    if h != cache.hkv:
+        _fail(f"k has {h} heads, the cache {cache.hkv}")
+    _table(table, b)
+    _check_shape(start, (b,), torch.int32, "start")
+    _check_shape(count, (b,), torch.int32, "count")
+    if (pos is None) != (rotary is None):
+        _fail("pos and rotary go together")
+    if rotary is not None:
+        _positions(pos, rotary, b, n, k.dim())
+    _on_vectors_device(k=k, v=v)
+    _here(table=table, start=start, count=count, pos=pos, cache=cache.k)
+    _check(lib().xattn_cache_append(_ptr(k), ks, _ptr(v), vs, b, n, _ptr(count), _ptr(start),
+                                    _ptr(table), table.shape[1], _ptr(pos),
+                                    None if rotary is None else rotary._ref, cache._ref,
+                                    _handle(stream)))
+
+
+def decode_workspace_size(cache: KVCache, batch: int, hq: int, table_pages: int,
+                          weights: bool = False) -> int:
+    """Bytes of xattn_decode's workspace."""
+    _is_cache(cache)
+    n = ctypes.c_size_t(0)
+    _check(lib().xattn_decode_workspace_size(cache._ref, batch, hq, table_pages,
+                                             int(bool(weights)), ctypes.byref(n)))
+    return n.value
+
+
+def xattn_decode(q, cache: KVCache, table, lens, o=None, lse=None, weights=None, workspace=None,
+                 want_lse=False, stream=None):
+    """Attention of one new token per sequence, q bf16 [batch, hq, 128], over its lens[b] cached
+    tokens: (o like q, lse fp32 [batch, hq] or None). weights (fp32 [batch, hkv,
+    table_pages * page]), if given, grow by each key's softmax weights, summed over its heads."""
+    _is_cache(cache)
+    if q.dim() != 3 or q.shape[2] != HEAD_DIM or 0 in q.shape:
+        _fail(f"q must be [batch, hq, {HEAD_DIM}], got {tuple(q.shape)}")
+    if q.dtype != torch.bfloat16:
+        _fail(f"q must be torch.bfloat16, got {q.dtype}")
+    b, hq, _ = q.shape
+    _table(table, b)
+    _check_shape(lens, (b,), torch.int32, "lens")
+    _check_shape(o, q.shape, torch.bfloat16, "o")
+    _check_shape(lse, (b, hq), torch.float32, "lse")
+    width = table.shape[1]
+    _check_shape(weights, (b, cache.hkv, width * cache.page), torch.float32, "weights")
+    _check_workspace(workspace)
+    _here(q=q, table=table, lens=lens, cache=cache.k, o=o, lse=lse, weights=weights,
+          workspace=workspace)
+    if o is None or workspace is None or (lse is None and want_lse):
+        with _allocating(stream):
+            if o is None:
+                o = torch.empty_like(q)
+            if lse is None and want_lse:
+                lse = torch.empty((b, hq), dtype=torch.float32, device=q.device)
+            if workspace is None:
+                need = decode_workspace_size(cache, b, hq, width, weights is not None)
+                workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _check(lib().xattn_decode(_ptr(q), cache._ref, b, hq, _ptr(table), width, _ptr(lens), _ptr(o),
+                              _ptr(lse), _ptr(weights), _ptr(workspace), workspace.numel(),
+                              _handle(stream)))
+    return o, lse
+
+
+def xattn_cache_evict(cache: KVCache, table, lens, weights, new_table, budget: int, recent: int,
+                      kept=None, new_lens=None, new_weights=None, stream=None):
+    """Moves the `budget` most valuable tokens of every sequence and key head (the last `recent`
+    and the heaviest before them) to the pages of new_table, none of which is in table. Returns
+    (kept int32 [batch, hkv, budget], new_lens int32 [batch], new_weights fp32 [batch, hkv,
+    new_pages * page])."""
+    _is_cache(cache)
+    if table.dim() != 2:
+        _fail(f"table must be [batch, pages], got {tuple(table.shape)}")
+    b, h, width, budget = table.shape[0], cache.hkv, table.shape[1], int(budget)
+    _table(table, b)
+    _table(new_table, b, "new_table")
+    _check_shape(lens, (b,), torch.int32, "lens")
+    _check_shape(weights, (b, h, width * cache.page), torch.float32, "weights")
+    new_width = new_table.shape[1]
+    if not 1 <= budget <= new_width * cache.page:
+        _fail(f"budget must be 1 to {new_width * cache.page} (the new table's tokens), got "
+              f"{budget}")
+    _check_shape(kept, (b, h, budget), torch.int32, "kept")
+    _check_shape(new_lens, (b,), torch.int32, "new_lens")
+    _check_shape(new_weights, (b, h, new_width * cache.page), torch.float32, "new_weights")
+    _here(table=table, lens=lens, weights=weights, new_table=new_table, cache=cache.k, kept=kept,
+          new_lens=new_lens, new_weights=new_weights)
+    for n, out, given in (("new_lens", new_lens, lens), ("new_weights", new_weights, weights)):
+        if out is not None and not _apart(out, given):
+            _fail(f"{n} must lie apart from the call's input")
+    if kept is None or new_lens is None or new_weights is None:
+        with _allocating(stream):
+            at = table.device
+            if kept is None:
+                kept = torch.empty((b, h, budget), dtype=torch.int32, device=at)
+            if new_lens is None:
+                new_lens = torch.empty((b,), dtype=torch.int32, device=at)
+            if new_weights is None:
+                new_weights = torch.empty((b, h, new_width * cache.page), dtype=torch.float32,
+                                          device=at)
+    _check(lib().xattn_cache_evict(cache._ref, b, _ptr(table), width, _ptr(lens), _ptr(weights),
+                                   budget, int(recent), _ptr(new_table), new_width, _ptr(kept),
+                                   _ptr(new_lens), _ptr(new_weights), _handle(stream)))
+    return kept, new_lens, new_weights
