@@ -4,12 +4,15 @@
 // A wave takes 16 keys of a key head against up to 16 of its query heads:
 //   S^T = K Q^T  by 16x16x32 bf16 MFMAs: lane (g, c) = (lane / 16, lane % 16)
 //     supplies K's row c and Q's row c, and receives queries c, keys 4g .. 4g+3;
-//   O^T += V^T P^T  by 16x16x4 fp32 MFMAs: step r takes the keys {4g + r}, so
-//     that P stays in the registers where the softmax left it, and the lane's
-//     piece of V is 8 consecutive values of row 4g + r: the i-th of them is row c
-//     of the A operand of MFMA i, whose output rows are elements 8c + i.
-// Neither K, V nor P passes through LDS, nothing is transposed, and P and the
-// values are fp32 in the second product.
+//   O^T += V^T P^T  by 16x16x32 bf16 MFMAs over two tiles: P stays in the lane
+//     where the softmax left it (keys 4g .. 4g+3 of both tiles are the lane's 8
+//     values of the contraction), and of V the lane loads elements 8c .. 8c+7 of
+//     those same keys, so that the i-th elements of its 8 pieces are row c of the
+//     A operand of MFMA i, whose output rows are elements 8c + i: pairs of values
+//     are put together within the lane, nothing moves between lanes.
+// P is the sum of two bf16 values (16 bits of mantissa, products exact), one MFMA
+// each: the product is as good as fp32 for an output in bf16, at an eighth of
+// the time of fp32 MFMAs.
 //
 // The work of a batch is its rows (sequence, key head, tile of query heads) end
 // to end, in units of kWaves wave steps; every workgroup takes an equal share of
@@ -30,19 +33,11 @@ constexpr int kRows = 16;  // query heads of a tile
 constexpr float kScale = 0.08838834764831845f * kLog2e;  // to log2, 1 / sqrt(128)
 constexpr float kMinusInf = -__builtin_inff();
 
-// Tiles of a wave's step: 16 KB of keys and values in either type.
-template <bool E4M3>
-constexpr int kTiles = E4M3 ? 2 : 2;
-
-__host__ __device__ constexpr int unit_keys(bool e4m3) {
-  return kTile * kWaves * (e4m3 ? 2 : 2);
-}
+constexpr int kTiles = 2;  // of a wave's step: the 32 keys of a PV MFMA
+constexpr int kUnit = kTile * kTiles * kWaves;
 
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x4 mfma4(float a, float b, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 __device__ __forceinline__ float scale_of(uint32_t byte) {
   return __builtin_bit_cast(float, byte << 23);
@@ -55,24 +50,37 @@ __device__ __forceinline__ bf16x8 bf16_of(uint32_t a, uint32_t b) {
   const auto s = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true);
   return bf16x8{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
 }
-// A lane's piece of a value vector in fp32.
-__device__ __forceinline__ void values(u32x4 u, float* f) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    f[2 * e] = __builtin_bit_cast(float, u[e] << 16);
-    f[2 * e + 1] = __builtin_bit_cast(float, u[e] & 0xffff0000u);
-  }
+// The two bf16 values of p and q whose sums they are: the upper halves of their
+// bits, and what is left, rounded. The rest is made 2^-17 p too large, so that it
+// is positive and an infinite value times p is infinite.
+__device__ __forceinline__ void split(float p, float q, uint32_t* upper, uint32_t* rest) {
+  const uint32_t a = __builtin_bit_cast(uint32_t, p), b = __builtin_bit_cast(uint32_t, q);
+  constexpr float kMore = 1.f + 0x1p-17f;
+  typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+  const bf16x2 r = {
+      (__bf16)__builtin_fmaf(p, kMore, -__builtin_bit_cast(float, a & 0xffff0000u)),
+      (__bf16)__builtin_fmaf(q, kMore, -__builtin_bit_cast(float, b & 0xffff0000u))};
+  *upper = __builtin_amdgcn_perm(b, a, 0x07060302u);
+  *rest = __builtin_bit_cast(uint32_t, r);
 }
-__device__ __forceinline__ void values(u32x2 u, float* f) {
-#pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(u[e], false);
-    const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8(u[e], true);
-    f[4 * e] = lo[0];
-    f[4 * e + 1] = lo[1];
-    f[4 * e + 2] = hi[0];
-    f[4 * e + 3] = hi[1];
-  }
+// Elements 2n and 2n + 1 (n = 0 .. 3) of a lane's four rows of a tile, in bf16:
+// rows 0, 1 and rows 2, 3 of the one, then of the other.
+__device__ __forceinline__ void columns(const u32x4* v, int n, uint32_t* even, uint32_t* odd) {
+  even[0] = __builtin_amdgcn_perm(v[1][n], v[0][n], 0x05040100u);
+  even[1] = __builtin_amdgcn_perm(v[3][n], v[2][n], 0x05040100u);
+  odd[0] = __builtin_amdgcn_perm(v[1][n], v[0][n], 0x07060302u);
+  odd[1] = __builtin_amdgcn_perm(v[3][n], v[2][n], 0x07060302u);
+}
+__device__ __forceinline__ void columns(const u32x2* v, int n, uint32_t* even, uint32_t* odd) {
+  // bytes 2n, 2n + 1 of rows 0, 1 and of rows 2, 3: of the one, then of the other
+  const uint32_t pick = n % 2 ? 0x07030602u : 0x05010400u;
+  const uint32_t a = __builtin_amdgcn_perm(v[1][n / 2], v[0][n / 2], pick);
+  const uint32_t b = __builtin_amdgcn_perm(v[3][n / 2], v[2][n / 2], pick);
+  const auto bits = [](auto x) { return __builtin_bit_cast(uint32_t, x); };
+  even[0] = bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, false));
+  even[1] = bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, false));
+  odd[0] = bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, true));
+  odd[1] = bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true));
 }
 // 2^(m - top) of a part whose maximum is m: nothing if it has summed nothing.
 __device__ __forceinline__ float weight_of(float m, float top) {
@@ -87,10 +95,6 @@ __device__ __forceinline__ int fresh(int x) {
 }
 // A value that is the same in every lane, for the compiler to see.
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ long long uniform(long long x) {
-  return (long long)(((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32) |
-                     (uint32_t)uniform((int)x));
-}
 
 struct DecodeParams {
   CacheParams c;
@@ -98,10 +102,10 @@ struct DecodeParams {
   const int32_t* lens;
   uint16_t* o;
   float* lse;    // or NULL
-  int batch, hq, group, row_tiles, tile_rows, unit, most_workers;
+  int batch, hq, group, row_tiles, tile_rows, most_workers;
   float* part;   // [2 workers][tile_rows][128] unnormalised outputs
   float* ml;     // [2 workers][tile_rows][2] (maximum in log2, sum)
-  float* stat;   // [batch][hq][2] (maximum in log2, 1 / sum), or NULL
+  float* stat;   // [batch][hq][2] (maximum in log2, sum) of whole rows, or NULL
   float* z;      // [batch][hq][capacity] products in log2, or NULL
 };
 
@@ -114,45 +118,37 @@ struct PieceOf<true> {
   typedef u32x2 type;
 };
 
-// Units that a workgroup is to have before there are more workgroups.
-constexpr int kLeastUnits = 1;
+// Workgroups that share a batch's units: three a CU, as many as are resident.
+constexpr int kMostWorkers = 768;
 
-__device__ __forceinline__ int workers_of(long long units, int most) {
-  const long long w = (units + kLeastUnits - 1) / kLeastUnits;
-  return w < most ? (int)w : most;
-}
-// First unit of a worker's share.
-__device__ __forceinline__ long long share(long long worker, long long units, int workers) {
-  return worker * units / workers;
-}
+// How `units` are shared out: the first `more` workgroups have per + 1 of them,
+// the others per; no more workgroups than units.
+struct Shares {
+  int workers, per, more;
+  __device__ Shares(int units, int most) {
+    workers = units < most ? units : most;
+    per = workers ? units / workers : 0;
+    more = units - workers * per;
+  }
+  __device__ int first(int worker) const { return worker * per + min(worker, more); }
+  __device__ int worker_of(int unit) const {
+    const int early = more * (per + 1);
+    return unit < early ? unit / (per + 1) : more + (unit - early) / per;
+  }
+};
 
 __device__ __forceinline__ int len_of(const DecodeParams& p, int b) {
   return clamp_len(p.lens[b], p.c.capacity());
 }
+// Units of a sequence's rows (all of its key heads and tiles of heads).
 __device__ __forceinline__ int units_of(const DecodeParams& p, int b) {
-  return (len_of(p, b) + p.unit - 1) / p.unit;
+  return (len_of(p, b) + kUnit - 1) / kUnit * (p.c.hkv * p.row_tiles);
 }
 
-// Sum over the workgroup's threads below this one, and over all of them.
-__device__ __forceinline__ long long scan(long long x, long long* total, long long* lds) {
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  long long y = x;
+__device__ __forceinline__ int sum_of_wave(int x) {
 #pragma unroll
-  for (int off = 1; off < kWave; off <<= 1) {
-    const long long up = __shfl_up(y, off);
-    if (lane >= off) y += up;
-  }
-  if (lane == kWave - 1) lds[wave] = y;
-  __syncthreads();
-  long long before = y - x, all = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) before += lds[w];
-    all += lds[w];
-  }
-  __syncthreads();
-  *total = all;
-  return before;
+  for (int off = 1; off < kWave; off <<= 1) x += __shfl_xor(x, off);
+  return x;
 }
 
 // One element of a finished row: output head `head`, element d.
@@ -164,20 +160,18 @@ __device__ __forceinline__ void write_row(const DecodeParams& p, long long head,
   if (d != 0) return;
   if (p.lse) p.lse[head] = sum == 0.f ? kMinusInf : (top + log2f(sum)) / kLog2e;
   if (p.stat) {
-    p.stat[2 * head] = sum == 0.f ? 0.f : top;
-    p.stat[2 * head + 1] = inv;
+    p.stat[2 * head] = top;
+    p.stat[2 * head + 1] = sum;
   }
 }
 
 template <bool E4M3, int RT>
 __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(DecodeParams p) {
-  constexpr int TILES = kTiles<E4M3>, KP = E4M3 ? 2 : 4;  // 16-byte pieces of a lane's key
+  constexpr int TILES = kTiles, KP = E4M3 ? 2 : 4;  // 16-byte pieces of a lane's key
   constexpr int STEP = TILES * kTile;
   using Piece = typename PieceOf<E4M3>::type;  // 8 values
   __shared__ float so[kWaves][RT * kRows][kHeadDim + 4];
   __shared__ float sm[kWaves][RT * kRows], sl[kWaves][RT * kRows];
-  __shared__ long long places[kWaves];
-  __shared__ long long found[2];
   const int tid = threadIdx.x, lane = tid % kWave;
   const unsigned g = lane / 16, c = lane % 16;
   // the lane's piece of a tile's keys and values, bytes
@@ -186,52 +180,42 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(Decod
   const int wave = uniform(tid / kWave);
   const int per_seq = p.c.hkv * p.row_tiles;
 
-  // this workgroup's share, and the sequence that it begins in
-  long long units = 0, first_before = 0;
-  for (int b0 = 0; b0 < p.batch; b0 += kThreads) {
-    const int b = b0 + tid;
-    long long all;
-    const long long before =
-        scan(b < p.batch ? (long long)units_of(p, b) * per_seq : 0, &all, places);
-    if (b0 == 0) first_before = before;
-    units += all;
+  // This workgroup's share, and the sequence that it begins in. Every wave finds
+  // out for itself, without a barrier: its lanes have equal runs of the batch.
+  const int run = (p.batch + kWave - 1) / kWave;
+  const int b0 = min(lane * run, p.batch), b1 = min(b0 + run, p.batch);
+  int mine = 0;
+  for (int i = b0; i < b1; ++i) mine += units_of(p, i);
+  int before = mine;
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1) {
+    const int up = __shfl_up(before, off);
+    if (lane >= off) before += up;
   }
-  units = uniform(units);
-  const int workers = workers_of(units, p.most_workers);
-  if ((int)blockIdx.x >= workers) return;
-  const long long begin = share(blockIdx.x, units, workers);
-  const long long end = share(blockIdx.x + 1, units, workers);
-  long long running = 0;
-  for (int b0 = 0; b0 < p.batch; b0 += kThreads) {
-    const int b = b0 + tid;
-    const long long mine = b < p.batch ? (long long)units_of(p, b) * per_seq : 0;
-    long long all = 0, before = first_before;
-    if (p.batch > kThreads) before = scan(mine, &all, places);
-    before += running;
-    if (before <= begin && begin < before + mine) {
-      found[0] = b;
-      found[1] = before;
-    }
-    running += all;
-  }
-  __syncthreads();
-  int b = uniform((int)found[0]);
-  long long at = begin - uniform(found[1]);  // units into sequence b
-  long long left = end - begin;
+  const Shares shares(__builtin_amdgcn_readlane(before, kWave - 1), p.most_workers);
+  if ((int)blockIdx.x >= shares.workers) return;
+  const int begin = shares.first(blockIdx.x);
+  int left = shares.first(blockIdx.x + 1) - begin;
+  const int holder = __ffsll((unsigned long long)__ballot(begin < before)) - 1;
+  int b = b0;
+  int at = begin - (before - mine);  // units into sequence b
+  if (lane == holder)
+    for (int u; at >= (u = units_of(p, b)); ++b) at -= u;
+  b = __builtin_amdgcn_readlane(b, holder);
+  at = __builtin_amdgcn_readlane(at, holder);
   bool first_segment = true;
 
   while (left > 0) {
     const int len = uniform(len_of(p, b));
-    const int row_units = (len + p.unit - 1) / p.unit;
-    if (row_units == 0 || at >= (long long)row_units * per_seq) {
+    const int row_units = (len + kUnit - 1) / kUnit;
+    if (at >= row_units * per_seq) {
       at = 0;
       ++b;
       continue;
     }
-    const int row = (int)(at / row_units), u0 = (int)(at - (long long)row * row_units);
-    const int n = (int)min(left, (long long)(row_units - u0));
+    const int row = at / row_units, u0 = at - row * row_units, n = min(left, row_units - u0);
     const int h = row / p.row_tiles, tile = row % p.row_tiles;
-    const int t0 = u0 * p.unit, t1 = min((u0 + n) * p.unit, len);
+    const int t0 = u0 * kUnit, t1 = min((u0 + n) * kUnit, len);
 
     bf16x8 q[RT][4];
     const int heads = p.group - tile * RT * kRows;  // of this row, if they are fewer than 16 RT
@@ -292,7 +276,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(Decod
       }
     };
     auto load_v = [&](const char* a, int i, int y) {
-      v[i][y] = *(const Piece*)(a + (E4M3 ? 128 : 256) * y + v_off);
+      v[i][y] = __builtin_nontemporal_load((const Piece*)(a + (E4M3 ? 128 : 256) * y + v_off));
     };
     auto load_scale = [&](long long r, int i) {
       if (E4M3) v_scale[i] = *(const uint32_t*)(p.c.v_scale + r + 4u * g);
@@ -398,32 +382,44 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(Decod
             l[x] += zs[x][i][r];
           }
       }
-      // the values; each of their registers takes the next step's piece as soon
-      // as it has been used
+      u32x4 upper[RT], rest[RT];
+#pragma unroll
+      for (int x = 0; x < RT; ++x)
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) {
+          if (E4M3)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) zs[x][i][r] *= scale_of(v_scale[i] >> (8 * r) & 255);
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            uint32_t a, b;
+            split(zs[x][i][2 * r], zs[x][i][2 * r + 1], &a, &b);
+            upper[x][2 * i + r] = a;
+            rest[x][2 * i + r] = b;
+          }
+        }
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        uint32_t e[4], f[4];
+        columns(v[0], n, e, f);
+        columns(v[1], n, e + 2, f + 2);
+        const bf16x8 even = as_bf16x8(u32x4{e[0], e[1], e[2], e[3]});
+        const bf16x8 odd = as_bf16x8(u32x4{f[0], f[1], f[2], f[3]});
+#pragma unroll
+        for (int x = 0; x < RT; ++x) {
+          o[x][2 * n] = mfma16(even, as_bf16x8(upper[x]), o[x][2 * n]);
+          o[x][2 * n + 1] = mfma16(odd, as_bf16x8(upper[x]), o[x][2 * n + 1]);
+          o[x][2 * n] = mfma16(even, as_bf16x8(rest[x]), o[x][2 * n]);
+          o[x][2 * n + 1] = mfma16(odd, as_bf16x8(rest[x]), o[x][2 * n + 1]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
 #pragma unroll
       for (int i = 0; i < TILES; ++i) {
         const long long row = place(next[i], t_next, i);
-        float pr[RT][4];
 #pragma unroll
-        for (int x = 0; x < RT; ++x)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            pr[x][r] = zs[x][i][r];
-            if (E4M3) pr[x][r] *= scale_of(v_scale[i] >> (8 * r) & 255);
-          }
+        for (int y = 0; y < 4; ++y) load_v((const char*)p.c.v + row * (E4M3 ? 128 : 256), i, y);
         load_scale(row, i);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          float f[8];
-          values(v[i][r], f);
-          __builtin_amdgcn_sched_barrier(0);
-          load_v((const char*)p.c.v + row * (E4M3 ? 128 : 256), i, r);
-#pragma unroll
-          for (int x = 0; x < RT; ++x)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) o[x][e] = mfma4(f[e], pr[x][r], o[x][e]);
-          __builtin_amdgcn_sched_barrier(0);
-        }
       }
 #pragma unroll
       for (int i = 0; i < TILES; ++i) now[i] = next[i];
@@ -484,96 +480,160 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(Decod
   }
 }
 
-// One workgroup per query head: the parts of its row, if it has any, eight at a
-// time, 32 lanes of 4 elements each, then the eight sums in order.
-__global__ __launch_bounds__(kThreads) void decode_join(DecodeParams p) {
-  constexpr int kLanes = kHeadDim / 4, kAtOnce = kThreads / kLanes;
-  __shared__ long long places[kWaves];
-  __shared__ float so[kAtOnce][kHeadDim];
-  __shared__ float sl[kAtOnce], st[kAtOnce];
-  const int tid = threadIdx.x, b = blockIdx.x / p.hq, hq = blockIdx.x % p.hq;
-  const int h = hq / p.group, in_group = hq % p.group;
-  const int tile = in_group / p.tile_rows, r = in_group % p.tile_rows;
-  const int per_seq = p.c.hkv * p.row_tiles;
-  long long units = 0, before = 0;
-  for (int i = tid; i < p.batch; i += kThreads) {
-    const long long u = (long long)units_of(p, i) * per_seq;
-    units += u;
+// Where a row's parts lie: of workgroup `first` in its slot 0 or 1, of the
+// others up to `last` in slot 0; none where one workgroup had the whole row.
+struct Parts {
+  int first, last, slot;
+  __device__ long long at(int worker) const {
+    return 2ll * worker + (worker == first ? slot : 0);
+  }
+};
+
+// The parts of sequence b's row (key head and tile of heads). Every wave for itself.
+__device__ __forceinline__ Parts parts_of(const DecodeParams& p, int b, int row) {
+  int all = 0, before = 0;
+  for (int i = threadIdx.x % kWave; i < p.batch; i += kWave) {
+    const int u = units_of(p, i);
+    all += u;
     if (i < b) before += u;
   }
-  long long all, all_before;
-  scan(units, &all, places);
-  scan(before, &all_before, places);
-  const int row_units = units_of(p, b);
-  if (row_units == 0) {
-    if (tid < kHeadDim) write_row(p, blockIdx.x, tid, 0.f, 0.f, 0.f);
+  const Shares shares(uniform(sum_of_wave(all)), p.most_workers);
+  const int row_units = (len_of(p, b) + kUnit - 1) / kUnit;
+  const int start = uniform(sum_of_wave(before)) + row * row_units;
+  Parts r;
+  r.first = shares.worker_of(start);
+  r.last = shares.worker_of(start + row_units - 1);
+  r.slot = shares.first(r.first) < start;
+  return r;
+}
+
+// One workgroup per query head: the parts of its row, if it has any, eight at a
+// time, 32 lanes of 4 elements each, then the eight sums in order.
+__device__ __forceinline__ void join(const DecodeParams& p, int head) {
+  constexpr int kLanes = kHeadDim / 4, kAtOnce = kThreads / kLanes;
+  __shared__ float so[kAtOnce][kHeadDim];
+  __shared__ float sf[kMostWorkers], sl[kMostWorkers], st[kWaves];
+  const int tid = threadIdx.x, b = head / p.hq, hq = head % p.hq;
+  const int h = hq / p.group, in_group = hq % p.group;
+  const int tile = in_group / p.tile_rows, r = in_group % p.tile_rows;
+  if (len_of(p, b) == 0) {
+    if (tid < kHeadDim) write_row(p, head, tid, 0.f, 0.f, 0.f);
     return;
   }
-  const int workers = workers_of(all, p.most_workers);
-  const long long start = all_before + (long long)(h * p.row_tiles + tile) * row_units;
-  const long long stop = start + row_units;
-  // the first worker whose share reaches past a unit u: share(w + 1) > u
-  auto worker_at = [&](long long u) {
-    long long w = u * workers / all;
-    while (share(w + 1, all, workers) <= u) ++w;
-    while (share(w, all, workers) > u) --w;
-    return (int)w;
-  };
-  const int w0 = worker_at(start), w1 = worker_at(stop - 1);
-  if (w0 == w1) return;  // written by decode_kernel
-  // in the first worker the row is its last one, unless it is also its first
-  auto slot_of = [&](int w) {
-    return 2ll * w + (w == w0 && share(w, all, workers) < start ? 1 : 0);
-  };
-  const int part = tid / kLanes, d = tid % kLanes * 4;
+  const Parts parts = parts_of(p, b, h * p.row_tiles + tile);
+  const int n = parts.last - parts.first + 1;
+  if (n == 1) return;  // written by decode_kernel
+  const int lane = tid % kWave, wave = tid / kWave;
   float top = kMinusInf;
-  for (int w = w0 + part; w <= w1; w += kAtOnce)
-    top = fmaxf(top, p.ml[(slot_of(w) * p.tile_rows + r) * 2]);
-  if (d == 0) st[part] = top;
+  for (int i = tid; i < n; i += kThreads) {
+    const float* ml = p.ml + (parts.at(parts.first + i) * p.tile_rows + r) * 2;
+    sf[i] = ml[0];
+    sl[i] = ml[1];
+    top = fmaxf(top, ml[0]);
+  }
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1) top = fmaxf(top, __shfl_xor(top, off));
+  if (lane == 0) st[wave] = top;
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kAtOnce; ++i) top = fmaxf(top, st[i]);
-  f32x4 out = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < kWaves; ++i) top = fmaxf(top, st[i]);
   float sum = 0.f;
-#pragma unroll 4
-  for (int w = w0 + part; w <= w1; w += kAtOnce) {
-    const long long at = slot_of(w) * p.tile_rows + r;
-    const float f = weight_of(p.ml[at * 2], top);
-    const f32x4 x = *(const f32x4*)(p.part + at * kHeadDim + d);
-    sum += f * p.ml[at * 2 + 1];
-    out += f * x;
+  for (int i = tid; i < n; i += kThreads) {
+    sf[i] = weight_of(sf[i], top);
+    sum += sf[i] * sl[i];
+  }
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1) sum += __shfl_xor(sum, off);
+  __syncthreads();
+  if (lane == 0) st[wave] = sum;
+  const int part = tid / kLanes, d = tid % kLanes * 4;
+  f32x4 out = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int i = part; i < n; i += kAtOnce) {
+    const long long at = parts.at(parts.first + i) * p.tile_rows + r;
+    out += sf[i] * *(const f32x4*)(p.part + at * kHeadDim + d);
   }
   *(f32x4*)&so[part][d] = out;
-  if (d == 0) sl[part] = sum;
   __syncthreads();
   if (tid >= kHeadDim) return;
-  float o = 0.f, s = 0.f;
+  float o = 0.f;
 #pragma unroll
-  for (int i = 0; i < kAtOnce; ++i) {
-    o += so[i][tid];
-    s += sl[i];
-  }
-  write_row(p, blockIdx.x, tid, top, s, o);
+  for (int i = 0; i < kAtOnce; ++i) o += so[i][tid];
+  sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) sum += st[i];
+  write_row(p, head, tid, top, sum, o);
 }
 
-// One thread per key: the weights of its group's heads, from the products.
-__global__ __launch_bounds__(kThreads) void decode_weights(DecodeParams p,
-                                                           float* __restrict__ weights) {
-  const int capacity = p.c.capacity(), chunks = (capacity + kThreads - 1) / kThreads;
-  const int row = blockIdx.x / chunks, t = blockIdx.x % chunks * kThreads + threadIdx.x;
-  const int b = row / p.c.hkv, h = row % p.c.hkv;
-  if (t >= clamp_len(p.lens[b], capacity)) return;
-  const long long first = (long long)b * p.hq + h * p.group;
-  float w = 0.f;
-  for (int i = 0; i < p.group; ++i) {
-    const float* st = p.stat + 2 * (first + i);
-    w += fast_exp2(p.z[(first + i) * capacity + t] - st[0]) * st[1];
+constexpr int kWeightKeys = 4 * kThreads;  // keys of a workgroup's weights
+
+// The weights of 1024 keys of a key head, from the products, a tile of its heads
+// after the other. First the heads' maxima and sums, eight lanes a head.
+__device__ __forceinline__ void add_weights(const DecodeParams& p, int chunk, int seq_head,
+                                            float* __restrict__ weights) {
+  __shared__ float stat[2 * kRows][2];
+  const int r = threadIdx.x / 8, sub = threadIdx.x % 8;
+  const int b = seq_head / p.c.hkv, h = seq_head % p.c.hkv, capacity = p.c.capacity();
+  const int len = len_of(p, b), t = chunk * kWeightKeys + 4 * (int)threadIdx.x;
+  if (chunk * kWeightKeys >= len) return;
+  f32x4 w = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int tile = 0; tile < p.row_tiles; ++tile) {
+    const int heads = min(p.tile_rows, p.group - tile * p.tile_rows);
+    const long long first = (long long)b * p.hq + h * p.group + tile * p.tile_rows;
+    const Parts parts = parts_of(p, b, h * p.row_tiles + tile);
+    float top = kMinusInf, sum = 0.f;
+    if (r < heads) {
+      if (parts.first == parts.last) {
+        top = p.stat[2 * (first + r)];
+        sum = sub == 0 ? p.stat[2 * (first + r) + 1] : 0.f;
+      } else {
+#pragma unroll 4
+        for (int x = parts.first + sub; x <= parts.last; x += 8) {
+          const float* ml = p.ml + (parts.at(x) * p.tile_rows + r) * 2;
+          const float m = ml[0], l = ml[1], to = fmaxf(top, m);
+          sum = sum * weight_of(top, to) + l * weight_of(m, to);
+          top = to;
+        }
+      }
+    }
+#pragma unroll
+    for (int off = 1; off < 8; off <<= 1) {
+      const float m = __shfl_xor(top, off), l = __shfl_xor(sum, off), to = fmaxf(top, m);
+      sum = sum * weight_of(top, to) + l * weight_of(m, to);
+      top = to;
+    }
+    __syncthreads();
+    if (sub == 0 && r < heads) {
+      stat[r][0] = sum == 0.f ? 0.f : top;
+      stat[r][1] = sum == 0.f ? 0.f : 1.f / sum;
+    }
+    __syncthreads();
+    if (t >= len) continue;
+    const float* z = p.z + first * capacity + t;
+#pragma unroll 8
+    for (int i = 0; i < heads; ++i) {
+      const f32x4 u = *(const f32x4*)(z + (size_t)i * capacity);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] += fast_exp2(u[e] - stat[i][0]) * stat[i][1];
+    }
   }
-  weights[(long long)row * capacity + t] += w;
+  if (t >= len) return;
+  float* to = weights + (long long)seq_head * capacity + t;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (t + e < len) to[e] += w[e];
 }
 
-// Workgroups that share a batch's units: three a CU, as many as are resident.
-constexpr int kMostWorkers = 768;
+// The first batch * hq workgroups join a head each; the others add the weights.
+__global__ __launch_bounds__(kThreads) void decode_join(DecodeParams p, int chunks,
+                                                        float* __restrict__ weights) {
+  const int heads = p.batch * p.hq, i = blockIdx.x;
+  if (i < heads)
+    join(p, i);
+  else
+    add_weights(p, (i - heads) % chunks, (i - heads) / chunks, weights);
+}
+
 
 size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
@@ -619,24 +679,21 @@ hipError_t launch_decode(const void* q, const CacheParams& c, bool e4m3, int bat
   p.group = hq / c.hkv;
   p.tile_rows = tile_rows_of(p.group);
   p.row_tiles = (p.group + p.tile_rows - 1) / p.tile_rows;
-  p.unit = unit_keys(e4m3);
   p.part = (float*)((char*)scratch + s.part);
   p.ml = (float*)((char*)scratch + s.ml);
   p.stat = weights ? (float*)((char*)scratch + s.stat) : nullptr;
   p.z = weights ? (float*)((char*)scratch + s.z) : nullptr;
   // no more workgroups than there can be units
   const long long most = (long long)batch * c.hkv * p.row_tiles *
-                         ((c.capacity() + p.unit - 1) / p.unit);
+                         ((c.capacity() + kUnit - 1) / kUnit);
   p.most_workers = most < kMostWorkers ? (int)most : kMostWorkers;
   auto* kernel = p.tile_rows <= kRows ? (e4m3 ? decode_kernel<true, 1> : decode_kernel<false, 1>)
                                       : (e4m3 ? decode_kernel<true, 2> : decode_kernel<false, 2>);
   hipLaunchKernelGGL(kernel, dim3(p.most_workers), dim3(kThreads), 0, st, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(decode_join, dim3(batch * hq), dim3(kThreads), 0, st, p);
-  if ((e = hipGetLastError()) != hipSuccess || !weights) return e;
-  const int chunks = (c.capacity() + kThreads - 1) / kThreads;
-  hipLaunchKernelGGL(decode_weights, dim3((unsigned)(batch * c.hkv * chunks)), dim3(kThreads), 0,
-                     st, p, weights);
+  const int chunks = weights ? (c.capacity() + kWeightKeys - 1) / kWeightKeys : 0;
+  hipLaunchKernelGGL(decode_join, dim3((unsigned)(batch * (hq + c.hkv * chunks))), dim3(kThreads),
+                     0, st, p, chunks, weights);
   return hipGetLastError();
 }
