@@ -15,6 +15,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 
 import numpy as np
 import torch
@@ -55,11 +56,9 @@ class Rotary:
         self.pairs, self.interleaved = tuple(pairs), bool(interleaved)
         self._plan = RotaryPlan(len(pairs), (ctypes.c_int32 * 3)(*pairs), int(self.interleaved),
                                 self._freq.ctypes.data)
+        self.axes = len(pairs)
         self._ref = ctypes.byref(self._plan)
 
-    @property
-    def axes(self) -> int:
-        return len(self.pairs)
 
 
 class KVCache:
@@ -106,55 +105,52 @@ class KVCache:
         return cls(*kv, *[zeros(pages, hkv, page, dtype=torch.uint8).fill_(127) for _ in "kv"])
 
 
-def _here(**tensors):
-    """Every tensor contiguous and on the current device, where the stream is."""
-    at = None
-    for n, t in tensors.items():
-        if t is None:
-            continue
-        if not t.is_cuda:
-            _fail(f"{n} must be a device tensor")
-        if not t.is_contiguous():
-            _fail(f"{n} must be contiguous")
-        if at is None:
-            at = torch.cuda.current_device()
-        if t.get_device() != at:
-            _fail(f"{n} must be on the current device {at}, got {t.device}")
+def _here(first, others, names, dense=()):
+    """Every tensor on the current device, where the stream is, and those of `dense` contiguous;
+    `names` are of (first, *others). Returns the device's index."""
+    at = first.get_device()
+    if at < 0:
+        _fail(f"{names[0]} must be a device tensor")
+    if at != torch._C._cuda_getDevice():
+        _fail(f"{names[0]} must be on the current device, got {first.device}")
+    for i, t in enumerate(others):
+        if t is not None and t.get_device() != at:
+            _fail(f"{names[i + 1]} must be a device tensor on {first.device}, got {t.device}")
+    for t in dense:
+        if t is not None and not t.is_contiguous():
+            at = [x is t for x in (first, *others)].index(True)
+            _fail(f"{names[at]} must be contiguous")
+    return at
+
+
+def _is(t, shape, dtype, name):
+    """_check_shape, at the cost of two comparisons where all is well."""
+    if t is not None and (t.shape != shape or t.dtype is not dtype):
+        _check_shape(t, shape, dtype, name)
 
 
 def _vectors(t, name, like=None):
     """(batch, heads, tokens, strides) of bf16 vectors, checked but for the device."""
     if t.dtype != torch.bfloat16:
         _fail(f"{name} must be torch.bfloat16, got {t.dtype}")
-    shape, strides = tuple(t.shape), t.stride()
+    shape, strides = t.shape, t.stride()
     if len(shape) == 3:
         shape, strides = (1, *shape), (0, *strides)
     if len(shape) != 4 or shape[3] != HEAD_DIM or 0 in shape:
         _fail(f"{name} must be [batch, heads, tokens, {HEAD_DIM}] or [heads, tokens, {HEAD_DIM}], "
               f"got {tuple(t.shape)}")
-    if like is not None and tuple(t.shape) != tuple(like.shape):
+    if like is not None and t.shape != like.shape:
         _fail(f"{name} must have shape {tuple(like.shape)}, got {tuple(t.shape)}")
     if strides[3] != 1:
         _fail(f"the {HEAD_DIM} values of a vector of {name} must be contiguous")
     return shape[0], shape[1], shape[2], _I3(*strides[:3])
 
 
-def _on_vectors_device(**tensors):
-    at = None
-    for n, t in tensors.items():
-        if not t.is_cuda:
-            _fail(f"{n} must be a device tensor")
-        if at is None:
-            at = torch.cuda.current_device()
-        if t.get_device() != at:
-            _fail(f"{n} must be on the current device {at}, got {t.device}")
-
-
 def _positions(pos, rotary, batch, tokens, dims):
     if not isinstance(rotary, Rotary):
         _fail(f"rotary must be a Rotary, got {type(rotary).__name__}")
-    shape = (rotary.axes, batch, tokens) if dims == 4 else (rotary.axes, tokens)
-    _check_shape(pos, shape, torch.int32, "pos")
+    _is(pos, (rotary.axes, batch, tokens) if dims == 4 else (rotary.axes, tokens), torch.int32,
+        "pos")
 
 
 def _is_cache(cache):
@@ -180,18 +176,13 @@ def _apart(a, b):
     return a1 <= b0 or b1 <= a0
 
 
-@contextlib.contextmanager
-def _nothing():
-    yield
-
-
 def _allocating(stream):
     """What a call allocates belongs to the stream that it runs on."""
-    return _nothing() if stream is None else torch.cuda.stream(stream)
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
-def _handle(stream):
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+def _handle(stream, at):
+    return torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream
 
 
 def xattn_rotary(x, pos, rotary: Rotary, inverse=False, out=None, stream=None):
@@ -199,21 +190,22 @@ def xattn_rotary(x, pos, rotary: Rotary, inverse=False, out=None, stream=None):
     [axes, batch, tokens] ([axes, tokens] for 3-D x). out: contiguous if not given; may be x."""
     b, h, n, xs = _vectors(x, "x")
     _positions(pos, rotary, b, n, x.dim())
-    if out is not None:
+    if out is None:
+        at = _here(x, (pos,), ("x", "pos"), (pos,))
+        if stream is None:
+            out = x.new_empty(x.shape)
+        else:
+            with _allocating(stream):
+                out = x.new_empty(x.shape)
+        os = _I3(h * n * HEAD_DIM, n * HEAD_DIM, HEAD_DIM)
+    else:
         _, _, _, os = _vectors(out, "out", x)
-        _on_vectors_device(x=x, out=out)
+        at = _here(x, (out, pos), ("x", "out", "pos"), (pos,))
         if not (out.data_ptr() == x.data_ptr() and out.stride() == x.stride()) \
                 and not _apart(out, x):
             _fail("out must be x itself or lie apart from it")
-    _on_vectors_device(x=x, pos=pos)
-    if not pos.is_contiguous():
-        _fail("pos must be contiguous")
-    if out is None:
-        with _allocating(stream):
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        os = _I3(h * n * HEAD_DIM, n * HEAD_DIM, HEAD_DIM)
-    _check(lib().xattn_rotary(_ptr(x), xs, b, h, n, HEAD_DIM, _ptr(pos), rotary._ref,
-                              int(bool(inverse)), _ptr(out), os, _handle(stream)))
+    _check(lib().xattn_rotary(x.data_ptr(), xs, b, h, n, HEAD_DIM, pos.data_ptr(), rotary._ref,
+                              1 if inverse else 0, out.data_ptr(), os, _handle(stream, at)))
     return out
 
 
@@ -227,28 +219,36 @@ def xattn_cache_append(k, v, cache: KVCache, table, start, count=None, pos=None,
     if h != cache.hkv:
         _fail(f"k has {h} heads, the cache {cache.hkv}")
     _table(table, b)
-    _check_shape(start, (b,), torch.int32, "start")
-    _check_shape(count, (b,), torch.int32, "count")
+    _is(start, (b,), torch.int32, "start")
+    _is(count, (b,), torch.int32, "count")
     if (pos is None) != (rotary is None):
         _fail("pos and rotary go together")
     if rotary is not None:
         _positions(pos, rotary, b, n, k.dim())
-    _on_vectors_device(k=k, v=v)
-    _here(table=table, start=start, count=count, pos=pos, cache=cache.k)
+    at = _here(k, (v, table, start, count, pos, cache.k),
+               ("k", "v", "table", "start", "count", "pos", "cache"), (table, start, count, pos))
     _check(lib().xattn_cache_append(_ptr(k), ks, _ptr(v), vs, b, n, _ptr(count), _ptr(start),
                                     _ptr(table), table.shape[1], _ptr(pos),
                                     None if rotary is None else rotary._ref, cache._ref,
-                                    _handle(stream)))
+                                    _handle(stream, at)))
+
+
+@functools.lru_cache(maxsize=256)
+def _decode_bytes(hkv, page, batch, hq, table_pages, weights):
+    """Workspace bytes of a shape; a function of the shape alone."""
+    c = Cache(1, page, hkv, HEAD_DIM, 0, None, None, None, None)
+    n = ctypes.c_size_t(0)
+    _check(lib().xattn_decode_workspace_size(ctypes.byref(c), batch, hq, table_pages, weights,
+                                             ctypes.byref(n)))
+    return n.value
 
 
 def decode_workspace_size(cache: KVCache, batch: int, hq: int, table_pages: int,
                           weights: bool = False) -> int:
     """Bytes of xattn_decode's workspace."""
     _is_cache(cache)
-    n = ctypes.c_size_t(0)
-    _check(lib().xattn_decode_workspace_size(cache._ref, batch, hq, table_pages,
-                                             int(bool(weights)), ctypes.byref(n)))
-    return n.value
+    return _decode_bytes(cache.hkv, cache.page, int(batch), int(hq), int(table_pages),
+                         int(bool(weights)))
 
 
 def xattn_decode(q, cache: KVCache, table, lens, o=None, lse=None, weights=None, workspace=None,
@@ -263,26 +263,26 @@ def xattn_decode(q, cache: KVCache, table, lens, o=None, lse=None, weights=None,
         _fail(f"q must be torch.bfloat16, got {q.dtype}")
     b, hq, _ = q.shape
     _table(table, b)
-    _check_shape(lens, (b,), torch.int32, "lens")
-    _check_shape(o, q.shape, torch.bfloat16, "o")
-    _check_shape(lse, (b, hq), torch.float32, "lse")
+    _is(lens, (b,), torch.int32, "lens")
+    _is(o, q.shape, torch.bfloat16, "o")
+    _is(lse, (b, hq), torch.float32, "lse")
     width = table.shape[1]
-    _check_shape(weights, (b, cache.hkv, width * cache.page), torch.float32, "weights")
+    _is(weights, (b, cache.hkv, width * cache.page), torch.float32, "weights")
     _check_workspace(workspace)
-    _here(q=q, table=table, lens=lens, cache=cache.k, o=o, lse=lse, weights=weights,
-          workspace=workspace)
-    if o is None or workspace is None or (lse is None and want_lse):
-        with _allocating(stream):
-            if o is None:
-                o = torch.empty_like(q)
-            if lse is None and want_lse:
-                lse = torch.empty((b, hq), dtype=torch.float32, device=q.device)
-            if workspace is None:
-                need = decode_workspace_size(cache, b, hq, width, weights is not None)
-                workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    dense = (q, table, lens, o, lse, weights, workspace)
+    at = _here(q, (table, lens, cache.k, o, lse, weights, workspace),
+               ("q", "table", "lens", "cache", "o", "lse", "weights", "workspace"), dense)
+    with _allocating(stream):
+        if o is None:
+            o = q.new_empty(q.shape)
+        if lse is None and want_lse:
+            lse = q.new_empty((b, hq), dtype=torch.float32)
+        if workspace is None:
+            need = _decode_bytes(cache.hkv, cache.page, b, hq, width, int(weights is not None))
+            workspace = q.new_empty((need,), dtype=torch.uint8)
     _check(lib().xattn_decode(_ptr(q), cache._ref, b, hq, _ptr(table), width, _ptr(lens), _ptr(o),
                               _ptr(lse), _ptr(weights), _ptr(workspace), workspace.numel(),
-                              _handle(stream)))
+                              _handle(stream, at)))
     return o, lse
 
 
@@ -298,31 +298,30 @@ def xattn_cache_evict(cache: KVCache, table, lens, weights, new_table, budget: i
     b, h, width, budget = table.shape[0], cache.hkv, table.shape[1], int(budget)
     _table(table, b)
     _table(new_table, b, "new_table")
-    _check_shape(lens, (b,), torch.int32, "lens")
-    _check_shape(weights, (b, h, width * cache.page), torch.float32, "weights")
+    _is(lens, (b,), torch.int32, "lens")
+    _is(weights, (b, h, width * cache.page), torch.float32, "weights")
     new_width = new_table.shape[1]
     if not 1 <= budget <= new_width * cache.page:
         _fail(f"budget must be 1 to {new_width * cache.page} (the new table's tokens), got "
               f"{budget}")
-    _check_shape(kept, (b, h, budget), torch.int32, "kept")
-    _check_shape(new_lens, (b,), torch.int32, "new_lens")
-    _check_shape(new_weights, (b, h, new_width * cache.page), torch.float32, "new_weights")
-    _here(table=table, lens=lens, weights=weights, new_table=new_table, cache=cache.k, kept=kept,
-          new_lens=new_lens, new_weights=new_weights)
+    _is(kept, (b, h, budget), torch.int32, "kept")
+    _is(new_lens, (b,), torch.int32, "new_lens")
+    _is(new_weights, (b, h, new_width * cache.page), torch.float32, "new_weights")
+    tensors = (lens, weights, new_table, kept, new_lens, new_weights)
+    at = _here(table, (*tensors, cache.k), ("table", "lens", "weights", "new_table", "kept",
+                                            "new_lens", "new_weights", "cache"),
+               (table, *tensors))
     for n, out, given in (("new_lens", new_lens, lens), ("new_weights", new_weights, weights)):
         if out is not None and not _apart(out, given):
             _fail(f"{n} must lie apart from the call's input")
-    if kept is None or new_lens is None or new_weights is None:
-        with _allocating(stream):
-            at = table.device
-            if kept is None:
-                kept = torch.empty((b, h, budget), dtype=torch.int32, device=at)
-            if new_lens is None:
-                new_lens = torch.empty((b,), dtype=torch.int32, device=at)
-            if new_weights is None:
-                new_weights = torch.empty((b, h, new_width * cache.page), dtype=torch.float32,
-                                          device=at)
+    with _allocating(stream):
+        if kept is None:
+            kept = lens.new_empty((b, h, budget))
+        if new_lens is None:
+            new_lens = lens.new_empty((b,))
+        if new_weights is None:
+            new_weights = weights.new_empty((b, h, new_width * cache.page))
     _check(lib().xattn_cache_evict(cache._ref, b, _ptr(table), width, _ptr(lens), _ptr(weights),
                                    budget, int(recent), _ptr(new_table), new_width, _ptr(kept),
-                                   _ptr(new_lens), _ptr(new_weights), _handle(stream)))
+                                   _ptr(new_lens), _ptr(new_weights), _handle(stream, at)))
     return kept, new_lens, new_weights
