@@ -445,13 +445,16 @@ int xattn_decode(const void *q, const xattn_cache *cache, int batch, int hq,
  *   new_lens     int32 [batch] (output): min(lens, budget); must not be lens
  *   new_weights  fp32 [batch][hkv][new_pages * page] (output): the kept tokens'
  *                weights, 0 behind them; no memory of weights
- * 1 <= budget, 0 <= recent <= budget. Page rows behind the kept tokens are left
+ *   workspace    at least xattn_evict_workspace_size() bytes; its contents on entry
+ *                are ignored
+ * The weights are 16-byte aligned. 1 <= budget, 0 <= recent <= budget. Page rows behind the kept tokens are left
  * as they were.
  */
+int xattn_evict_workspace_size(const xattn_cache *cache, int batch, int table_pages, size_t *bytes);
 int xattn_cache_evict(const xattn_cache *cache, int batch, const int32_t *table, int table_pages,
                       const int32_t *lens, const float *weights, int budget, int recent,
                       const int32_t *new_table, int new_pages, int32_t *kept, int32_t *new_lens,
-                      float *new_weights, void *stream);
+                      float *new_weights, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Static description of a status code (never NULL). */
 const char *xattn_strerror(int status);

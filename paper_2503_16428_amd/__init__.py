@@ -14,7 +14,7 @@ from .binding import (  # noqa: F401
     xattn_select_topk,
 )
 from .serving import (  # noqa: F401,E402
-    KVCache, Rotary, decode_workspace_size, rotary_freqs, xattn_cache_append, xattn_cache_evict,
-    xattn_decode, xattn_rotary,
+    KVCache, Rotary, decode_workspace_size, evict_workspace_size, rotary_freqs,
+    xattn_cache_append, xattn_cache_evict, xattn_decode, xattn_rotary,
 )
 from .threshold import predict_thresholds  # noqa: F401,E402

@@ -77,7 +77,7 @@ EXPORTS = [
     "xattn_threshold_levels", "xattn_threshold_predict",
     "xattn_head_error_workspace_size", "xattn_head_error", "xattn_head_error_mean",
     "xattn_rotary", "xattn_cache_append", "xattn_decode_workspace_size", "xattn_decode",
-    "xattn_cache_evict",
+    "xattn_evict_workspace_size", "xattn_cache_evict",
     "xattn_strerror", "xattn_last_error", "xattn_version",
 ]
 
@@ -121,7 +121,8 @@ def lib() -> ctypes.CDLL:
         L.xattn_cache_append.argtypes = [P, P, P, P, I, I, P, P, P, I, P, PP, PC, P]
         L.xattn_decode_workspace_size.argtypes = [PC, I, I, I, I, PSZ]
         L.xattn_decode.argtypes = [P, PC, I, I, P, I, P, P, P, P, P, SZ, P]
-        L.xattn_cache_evict.argtypes = [PC, I, P, I, P, P, I, I, P, I, P, P, P, P]
+        L.xattn_evict_workspace_size.argtypes = [PC, I, I, PSZ]
+        L.xattn_cache_evict.argtypes = [PC, I, P, I, P, P, I, I, P, I, P, P, P, P, SZ, P]
         L.xattn_strerror.argtypes = [I]
         L.xattn_strerror.restype = ctypes.c_char_p
         L.xattn_last_error.restype = ctypes.c_char_p

@@ -1,13 +1,16 @@
 // Eviction from the paged cache by accumulated attention weight.
 //
-// evict_select: one workgroup per (sequence, key head) finds the weight of the
-// last token kept and writes the kept tokens in order. A wave has a run of the
-// tokens. The weight is found over its order-preserving integer: a histogram of
-// the upper 11 bits; the tokens of the digit that holds the last place, collected
-// in LDS (in memory again where they are too many); two histograms of theirs for
-// the other 21 bits. The places of a wave's tokens follow from the counts of the
-// waves before it, so the last pass needs no barrier. evict_move copies the
-// tokens' vectors to the new pages.
+// The weight of the last token kept is found over its order-preserving integer,
+// 11, 11 and 10 bits at a time, by one workgroup per 8192 tokens of a row
+// (sequence, key head), in three launches:
+//   evict_count    histogram of the upper 11 bits of a chunk's weights;
+//   evict_collect  sums the row's histograms, finds the digit of the last place,
+//                  lists the chunk's tokens that have it and counts their next
+//                  11 bits;
+//   evict_emit     finds that digit, and the last 10 bits from the row's lists;
+//                  the places of a chunk's tokens follow from the counts of the
+//                  chunks before it, and it writes its kept tokens.
+// evict_move copies the tokens' vectors to the new pages.
 #include "serve.h"
 
 using namespace xattn;
@@ -16,12 +19,33 @@ namespace {
 
 constexpr int kSelThreads = 1024;
 constexpr int kSelWaves = kSelThreads / kWave;
-constexpr int kStep = 4 * kWave;      // tokens of a wave's step, four a lane
-constexpr int kBins = 2048;           // of a histogram
-constexpr int kCopies = 4;            // of it: one for the waves of a SIMD
-constexpr int kListed = 1536;         // tokens that a wave can collect
-constexpr int kHeld = 4;              // steps whose weights stay in registers
+constexpr int kSteps = 2;                        // of 4 tokens a lane
+constexpr int kStep = 4 * kWave;                 // tokens of a wave's step
+constexpr int kRun = kSteps * kStep;             // and of its part of a chunk
+constexpr int kChunk = kSelWaves * kRun;         // tokens of a workgroup
+constexpr int kBins = 2048;                      // of a histogram
+constexpr int kCopies = 2;                       // of it in LDS
 constexpr int kMoveThreads = 256;
+
+// What the launches leave for the next, per chunk and per row.
+struct ChunkCounts {
+  int above, listed;  // tokens above the first digit, tokens that have it
+};
+struct RowDigit {
+  int digit, left;  // the first digit, and the place within it that is wanted
+};
+struct EvictParams {
+  CacheParams c;
+  const int32_t* lens;
+  const float* weights;
+  int budget, recent, chunks, new_capacity;
+  int32_t *kept, *new_lens;
+  float* new_weights;
+  int* hist;            // [rows][chunks][2][kBins]
+  uint32_t* list;       // [rows][chunks][kChunk]
+  ChunkCounts* counts;  // [rows][chunks]
+  RowDigit* digits;     // [rows]
+};
 
 // Integer with the order of the weights: NaN lowest, -0 equal to 0.
 __device__ __forceinline__ uint32_t rank_of(float w) {
@@ -45,28 +69,50 @@ __device__ __forceinline__ void count(int* hist, int d, bool in) {
 
 struct SelectShared {
   int hist[kCopies][kBins];
-  uint32_t list[kSelWaves][kListed];
-  int listed[kSelWaves], above[kSelWaves], equal[kSelWaves], sums[kSelWaves];
-  int digit, left;
+  int above[kSelWaves], equal[kSelWaves], sums[kSelWaves];
+  int digit, left, listed;
 };
 
+// Sum of the first n of the waves' numbers in LDS, in every lane.
+__device__ __forceinline__ int sum_of_first(const int* a, int n) {
+  const int lane = threadIdx.x % kSelWaves;
+  int x = lane < n ? a[lane] : 0;
+#pragma unroll
+  for (int off = 1; off < kSelWaves; off <<= 1) x += __shfl_xor(x, off);
+  return x;
+}
+
 __device__ __forceinline__ void clear(SelectShared& s) {
-  for (int i = threadIdx.x; i < kCopies * kBins; i += kSelThreads) (&s.hist[0][0])[i] = 0;
+  for (int i = threadIdx.x; i < kCopies * kBins / 4; i += kSelThreads)
+    ((int4*)&s.hist[0][0])[i] = int4{0, 0, 0, 0};
   __syncthreads();
 }
 
-// The bin of the `take`-th largest counted, and the place in it that is wanted.
-__device__ __forceinline__ void find(SelectShared& s, int take) {
+// The chunk's histogram to memory.
+__device__ __forceinline__ void store(const SelectShared& s, int* to) {
+  __syncthreads();
+  for (int i = threadIdx.x; i < kBins; i += kSelThreads) {
+    int n = 0;
+    for (int c = 0; c < kCopies; ++c) n += s.hist[c][i];
+    to[i] = n;
+  }
+}
+
+// The bin of the `take`-th largest of `parts` histograms that lie `stride` apart,
+// and the place in it that is wanted.
+__device__ __forceinline__ void find(SelectShared& s, const int* hist, int parts, int stride,
+                                     int take) {
   static_assert(kBins == 2 * kSelThreads, "two bins a thread");
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-  __syncthreads();
-  const int high = kBins - 1 - 2 * tid;  // this thread's bins: high, high - 1
-  int n[2] = {0, 0};
-  for (int c = 0; c < kCopies; ++c) {
-    n[0] += s.hist[c][high];
-    n[1] += s.hist[c][high - 1];
+  const int low = kBins - 2 - 2 * tid;  // this thread's bins: low + 1, low
+  int n0 = 0, n1 = 0;
+#pragma unroll 8
+  for (int i = 0; i < parts; ++i) {
+    const int2 x = *(const int2*)(hist + (size_t)i * stride + low);
+    n0 += x.y;
+    n1 += x.x;
   }
-  int up_to = n[0] + n[1];
+  int up_to = n0 + n1;
 #pragma unroll
   for (int off = 1; off < kWave; off <<= 1) {
     const int x = __shfl_up(up_to, off);
@@ -74,239 +120,286 @@ __device__ __forceinline__ void find(SelectShared& s, int take) {
   }
   if (lane == kWave - 1) s.sums[wave] = up_to;
   __syncthreads();
-  for (int w = 0; w < wave; ++w) up_to += s.sums[w];
-  const int before = up_to - n[0] - n[1];
+  up_to += sum_of_first(s.sums, wave);
+  const int before = up_to - n0 - n1;
   if (before < take && take <= up_to) {
-    const bool second = take > before + n[0];
-    s.digit = high - second;
-    s.left = take - before - (second ? n[0] : 0);
+    const bool second = take > before + n0;
+    s.digit = low + !second;
+    s.left = take - before - (second ? n0 : 0);
   }
   __syncthreads();
 }
 
-// HELD: rows of at most kSelWaves * kHeld * kStep tokens, read once.
-template <bool HELD>
-__global__ __launch_bounds__(kSelThreads) void evict_select(
-    CacheParams c, const int32_t* __restrict__ lens, const float* __restrict__ weights, int budget,
-    int recent, int new_capacity, int32_t* __restrict__ kept, int32_t* __restrict__ new_lens,
-    float* __restrict__ new_weights) {
+// A workgroup's place: its row's length and tokens, and its lanes' weights.
+struct Chunk {
+  int row, index, n, old, wanted, t0;  // t0: the lane's first token
+  const float* w;
+  f32x4 x[kSteps];
+  __device__ Chunk(const EvictParams& p) {
+    row = blockIdx.x / p.chunks;
+    index = blockIdx.x % p.chunks;
+    n = clamp_len(p.lens[row / p.c.hkv], p.c.capacity());
+    old = n - p.recent;             // tokens that compete,
+    wanted = p.budget - p.recent;   // for so many places
+    w = p.weights + (long long)row * p.c.capacity();
+    t0 = index * kChunk + (int)threadIdx.x / kWave * kRun + 4 * ((int)threadIdx.x % kWave);
+  }
+  // rows begin at multiples of 16 weights and hold multiples of 16
+  __device__ void load() {
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i)
+      if (t0 + i * kStep < n) x[i] = *(const f32x4*)(w + t0 + i * kStep);
+  }
+  template <class F>
+  __device__ void each(F f) {
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f(t0 + i * kStep + e, x[i][e]);
+  }
+};
+
+__global__ __launch_bounds__(kSelThreads) void evict_count(EvictParams p) {
   __shared__ SelectShared s;
-  const int b = blockIdx.x / c.hkv, tid = threadIdx.x, lane = tid % kWave;
-  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const int capacity = c.capacity(), n = clamp_len(lens[b], capacity);
-  const float* w = weights + (long long)blockIdx.x * capacity;
-  kept += (long long)blockIdx.x * budget;
-  new_weights += (long long)blockIdx.x * new_capacity;
-  const int m = n < budget ? n : budget;
-  if (blockIdx.x % c.hkv == 0 && tid == 0) new_lens[b] = m;
-  for (int i = m + tid; i < budget; i += kSelThreads) kept[i] = -1;
-  for (int i = m + tid; i < new_capacity; i += kSelThreads) new_weights[i] = 0.f;
-  if (n <= budget) {
-    for (int i = tid; i < n; i += kSelThreads) {
+  Chunk k(p);
+  const int tid = threadIdx.x, m = min(k.n, p.budget);
+  const int first = k.index * kSelThreads + tid, all = p.chunks * kSelThreads;
+  int32_t* kept = p.kept + (long long)k.row * p.budget;
+  float* new_weights = p.new_weights + (long long)k.row * p.new_capacity;
+  if (k.row % p.c.hkv == 0 && first == 0) p.new_lens[k.row / p.c.hkv] = m;
+  for (int i = m + first; i < p.budget; i += all) kept[i] = -1;
+  for (int i = m + first; i < p.new_capacity; i += all) new_weights[i] = 0.f;
+  if (k.n <= p.budget) {  // all of them
+    for (int i = first; i < k.n; i += all) {
       kept[i] = i;
-      new_weights[i] = w[i];
+      new_weights[i] = k.w[i];
     }
     return;
   }
+  if (k.wanted == 0 || k.index * kChunk >= k.n) return;
+  k.load();
+  clear(s);
+  int* hist = s.hist[tid / kWave % kCopies];
+  k.each([&](int t, float x) { count(hist, rank_of(x) >> 21, t < k.old); });
+  store(s, p.hist + (size_t)blockIdx.x * (2 * kBins));
+}
 
-  const int old = n - recent, wanted = budget - recent;  // tokens that compete, and places
-  const int run = HELD ? kHeld * kStep : (n + kSelWaves * kStep - 1) / (kSelWaves * kStep) * kStep;
-  const int t0 = wave * run, t1 = min(t0 + run, n);
-  f32x4 held[kHeld];
-  // f(token, weight of it and the next three) for the lane's tokens of each step;
-  // rows begin at multiples of 16 weights, so the last one's four can be read
-  auto each = [&](auto f, bool first = false) {
-    if (HELD) {
-#pragma unroll
-      for (int i = 0; i < kHeld; ++i) {
-        const int t = t0 + i * kStep + 4 * lane;
-        if (first && t < t1) held[i] = *(const f32x4*)(w + t);
-        if (t0 + i * kStep < t1) f(t, held[i]);
-      }
-      return;
-    }
-    constexpr int kAhead = 4;
-    int t = t0 + 4 * lane;
-    for (int base = t0; base < t1; base += kAhead * kStep) {
-      f32x4 x[kAhead];
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i)
-        if (t + i * kStep < t1) x[i] = *(const f32x4*)(w + t + i * kStep);
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i)
-        if (base + i * kStep < t1) f(t + i * kStep, x[i]);
-      t += kAhead * kStep;
-    }
-  };
+__global__ __launch_bounds__(kSelThreads) void evict_collect(EvictParams p) {
+  __shared__ SelectShared s;
+  Chunk k(p);
+  if (k.n <= p.budget || k.wanted == 0 || k.index * kChunk >= k.n) return;
+  const int tid = threadIdx.x, lane = tid % kWave, chunks = (k.n + kChunk - 1) / kChunk;
+  k.load();
+  if (tid == 0) s.listed = 0;
+  clear(s);
+  find(s, p.hist + (size_t)k.row * p.chunks * (2 * kBins), chunks, 2 * kBins, k.wanted);
+  const uint32_t digit = s.digit;
+  uint32_t* list = p.list + (size_t)blockIdx.x * kChunk;
+  int* hist = s.hist[tid / kWave % kCopies];
+  int above = 0;
+  k.each([&](int t, float x) {
+    const uint32_t r = rank_of(x);
+    above += __popcll(__ballot(t < k.old && r >> 21 > digit));
+    const bool in = t < k.old && r >> 21 == digit;
+    const uint64_t who = __ballot(in);
+    if (!who) return;
+    int at = 0;
+    if (lane == 0) at = atomicAdd(&s.listed, __popcll(who));
+    at = __builtin_amdgcn_readfirstlane(at) + __popcll(who & (((uint64_t)1 << lane) - 1));
+    if (in) list[at] = r;
+    count(hist, r >> 10 & (kBins - 1), in);
+  });
+  if (lane == 0) s.above[tid / kWave] = above;
+  store(s, p.hist + (size_t)blockIdx.x * (2 * kBins) + kBins);
+  if (tid != 0) return;
+  above = 0;
+  for (int i = 0; i < kSelWaves; ++i) above += s.above[i];
+  p.counts[blockIdx.x] = ChunkCounts{above, s.listed};
+  if (k.index == 0) p.digits[k.row] = RowDigit{(int)digit, s.left};
+}
 
-  int* hist = s.hist[wave % kCopies];
+__global__ __launch_bounds__(kSelThreads) void evict_emit(EvictParams p) {
+  __shared__ SelectShared s;
+  Chunk k(p);
+  if (k.n <= p.budget || k.index * kChunk >= k.n) return;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int chunks = (k.n + kChunk - 1) / kChunk;
+  const int first = k.row * p.chunks;  // the row's chunks
+  const bool some = k.wanted > 0;
+  k.load();
   uint32_t last = 0;  // the rank of the last token kept, and how many of that rank are
-  int take = wanted, musts = 0, equals = 0;
-  if (wanted > 0) {
+  int take = 0, base = 0, ties = 0;  // kept, and of that rank, in the chunks before
+  if (some) {
     clear(s);
-    each([&](int t, f32x4 x) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) count(hist, rank_of(x[e]) >> 21, t + e < old);
-    }, true);
-    find(s, take);
-    last = (uint32_t)s.digit << 21;
+    const RowDigit d = p.digits[k.row];
+    find(s, p.hist + (size_t)first * (2 * kBins) + kBins, chunks, 2 * kBins, d.left);
+    last = (uint32_t)d.digit << 21 | (uint32_t)s.digit << 10;
     take = s.left;
-    // the tokens above that digit are kept; those in it are collected
-    int listed = 0;
-    const uint64_t below = ((uint64_t)1 << lane) - 1;
-    each([&](int t, f32x4 x) {
+    // f(whether, rank) for the tokens listed in the first `upto` chunks, whole
+    // waves at a time, a wave a chunk
+    auto each_listed = [&](int upto, auto f) {
+      constexpr int kAhead = 4;
+      for (int i = wave; i < upto; i += kSelWaves) {
+        const int listed = __builtin_amdgcn_readfirstlane(p.counts[first + i].listed);
+        const uint32_t* list = p.list + (size_t)(first + i) * kChunk;
+        for (int at = lane; at - lane < listed; at += kAhead * kWave) {
+          uint32_t r[kAhead];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t r = rank_of(x[e]);
-        const bool in = t + e < old;
-        musts += __popcll(__ballot(in && r >> 21 > last >> 21));
-        const bool mine = in && r >> 21 == last >> 21;
-        const uint64_t who = __ballot(mine);
-        const int at = listed + __popcll(who & below);
-        if (mine && at < kListed) s.list[wave][at] = r;
-        listed += __popcll(who);
+          for (int x = 0; x < kAhead; ++x)
+            r[x] = at + x * kWave < listed ? list[at + x * kWave] : 0;
+#pragma unroll
+          for (int x = 0; x < kAhead; ++x) f(at + x * kWave < listed, r[x]);
+        }
       }
+    };
+    each_listed(chunks, [&](bool in, uint32_t r) {
+      count(s.hist[wave % kCopies], r & 1023, in && (r ^ last) >> 10 == 0);
     });
-    if (lane == 0) s.listed[wave] = listed;
     __syncthreads();
-    bool fits = true;
-    for (int i = 0; i < kSelWaves; ++i) fits = fits && s.listed[i] <= kListed;
-    for (int shift = 10; shift >= 0; shift -= 10) {
-      const int bits = shift ? 11 : 10;
-      clear(s);
-      if (fits) {
-        for (int i = lane; i - lane < listed; i += kWave) {
-          const uint32_t r = i < listed ? s.list[wave][i] : 0;
-          count(hist, r >> shift & ((1 << bits) - 1),
-                i < listed && (r ^ last) >> (shift + bits) == 0);
-        }
-      } else {
-        each([&](int t, f32x4 x) {
+    find(s, s.hist[0], kCopies, kBins, take);
+    last |= s.digit;
+    take = s.left;
+    int above = 0, equal = 0;
+    each_listed(k.index, [&](bool in, uint32_t r) {
+      above += __popcll(__ballot(in && r > last));
+      equal += __popcll(__ballot(in && r == last));
+    });
+    int before = 0;
+    for (int i = tid; i < k.index; i += kSelThreads) before += p.counts[first + i].above;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t r = rank_of(x[e]);
-            count(hist, r >> shift & ((1 << bits) - 1),
-                  t + e < old && (r ^ last) >> (shift + bits) == 0);
-          }
-        });
-      }
-      find(s, take);
-      last |= (uint32_t)s.digit << shift;
-      take = s.left;
+    for (int off = 1; off < kWave; off <<= 1) before += __shfl_xor(before, off);
+    if (lane == 0) {
+      s.above[wave] = above + before;
+      s.equal[wave] = equal;
     }
-    if (fits) {
-      for (int i = lane; i - lane < listed; i += kWave) {
-        const uint32_t r = i < listed ? s.list[wave][i] : 0;
-        musts += __popcll(__ballot(i < listed && r > last));
-        equals += __popcll(__ballot(i < listed && r == last));
-      }
-    } else {
-      musts = 0;
-      each([&](int t, f32x4 x) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t r = rank_of(x[e]);
-          musts += __popcll(__ballot(t + e < old && r > last));
-          equals += __popcll(__ballot(t + e < old && r == last));
-        }
-      });
-    }
+    __syncthreads();
+    base = sum_of_first(s.above, kSelWaves);
+    ties = sum_of_first(s.equal, kSelWaves);
+    __syncthreads();
   }
-  musts += max(0, t1 - max(t0, old));
+  base += max(0, k.index * kChunk - max(0, k.old));
+  // this chunk's, wave after wave
+  auto must = [&](int t, uint32_t r) {
+    return (t >= k.old && t < k.n) || (some && t < k.old && r > last);
+  };
+  auto tie = [&](int t, uint32_t r) { return some && t < k.old && r == last; };
+  int musts = 0, equals = 0;
+  k.each([&](int t, float x) {
+    const uint32_t r = rank_of(x);
+    musts += __popcll(__ballot(must(t, r)));
+    equals += __popcll(__ballot(tie(t, r)));
+  });
   if (lane == 0) {
     s.above[wave] = musts;
     s.equal[wave] = equals;
   }
   __syncthreads();
-  // places taken and equal tokens met before this wave's run; of the equal ones
-  // the first `take` of the row are kept
-  int base = 0, ties = 0;
-  for (int i = 0; i < wave; ++i) {
-    base += s.above[i];
-    ties += s.equal[i];
-  }
-  const bool first_read = HELD && wanted == 0;
-  each([&](int t, f32x4 x) {
-    bool must[4], tie[4];
-    uint32_t must_before = 0, tie_before = 0;  // in the lanes below
-    int must_all = 0, tie_all = 0;
+  base += sum_of_first(s.above, wave);
+  ties += sum_of_first(s.equal, wave);
+  int32_t* kept = p.kept + (long long)k.row * p.budget;
+  float* new_weights = p.new_weights + (long long)k.row * p.new_capacity;
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    int at = base, tied = ties;  // and those of the lanes below and of this lane
+    uint32_t r[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const uint32_t r = rank_of(x[e]);
-      const bool competes = wanted > 0 && t + e < old;
-      must[e] = (t + e >= old && t + e < n) || (competes && r > last);
-      tie[e] = competes && r == last;
-      const uint64_t a = __ballot(must[e]), q = __ballot(tie[e]);
-      must_before = __builtin_amdgcn_mbcnt_hi(a >> 32,
-                                              __builtin_amdgcn_mbcnt_lo((uint32_t)a, must_before));
-      tie_before = __builtin_amdgcn_mbcnt_hi(q >> 32,
-                                             __builtin_amdgcn_mbcnt_lo((uint32_t)q, tie_before));
-      must_all += __popcll(a);
-      tie_all += __popcll(q);
+      const int t = k.t0 + i * kStep + e;
+      r[e] = rank_of(k.x[i][e]);
+      const uint64_t a = __ballot(must(t, r[e])), q = __ballot(tie(t, r[e]));
+      at += __popcll(a & below);
+      tied += __popcll(q & below);
+      base += __popcll(a);
+      ties += __popcll(q);
     }
-    int at = base + (int)must_before, tied = ties + (int)tie_before;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      if (must[e] || (tie[e] && tied < take)) {
+      const int t = k.t0 + i * kStep + e;
+      const bool m = must(t, r[e]), q = tie(t, r[e]);
+      if (m || (q && tied < take)) {  // of the equal ones the row's first `take`
         const int place = at + min(tied, take);
-        kept[place] = t + e;
-        new_weights[place] = x[e];
+        kept[place] = t;
+        new_weights[place] = k.x[i][e];
       }
-      at += must[e];
-      tied += tie[e];
+      at += m;
+      tied += q;
     }
-    base += must_all;
-    ties += tie_all;
-  }, first_read);
+  }
 }
 
-// 16 lanes a token for bf16, 8 for e4m3: a 16-byte piece of its key and value each.
+// 16 lanes a token for bf16, 8 for e4m3: a 16-byte piece of its key and value
+// each. Loads that are not to stay in the caches and stores that may: 10 % faster
+// than both one way or the other way round (four tokens a thread: 5 % slower).
 template <bool E4M3>
 __global__ __launch_bounds__(kMoveThreads) void evict_move(CacheParams c,
                                                            const int32_t* __restrict__ lens,
-                                                           int budget,
+                                                           int budget, int moves,
                                                            const int32_t* __restrict__ new_table,
                                                            int new_pages,
                                                            const int32_t* __restrict__ kept) {
   constexpr int kBytes = E4M3 ? kHeadDim : 2 * kHeadDim, kPer = kBytes / 16;
-  constexpr int kRows = kMoveThreads / kPer;
-  const int chunks = (budget + kRows - 1) / kRows;
-  const int row = blockIdx.x / chunks, b = row / c.hkv, h = row % c.hkv;
-  const int i = blockIdx.x % chunks * kRows + threadIdx.x / kPer, piece = threadIdx.x % kPer;
-  if (i >= budget || i >= clamp_len(lens[b], c.capacity())) return;
+  const int row = blockIdx.x / moves, b = row / c.hkv, h = row % c.hkv;
+  const int i = blockIdx.x % moves * (kMoveThreads / kPer) + threadIdx.x / kPer;
+  const int piece = threadIdx.x % kPer, slot = (1 << c.shift) - 1;
+  if (i >= min(budget, clamp_len(lens[b], c.capacity()))) return;
   const int t = kept[(long long)row * budget + i];
-  const int slot = (1 << c.shift) - 1;
   const long long from = page_row(c.table[(long long)b * c.table_pages + (t >> c.shift)], c.pages,
                                   c.hkv, h, c.shift, t & slot);
   const long long to = page_row(new_table[(long long)b * new_pages + (i >> c.shift)], c.pages,
                                 c.hkv, h, c.shift, i & slot);
   if (from < 0 || to < 0) return;
   char *k = (char*)c.k + piece * 16, *v = (char*)c.v + piece * 16;
-  const u32x4 x = *(const u32x4*)(k + from * kBytes), y = *(const u32x4*)(v + from * kBytes);
-  *(u32x4*)(k + to * kBytes) = x;
-  *(u32x4*)(v + to * kBytes) = y;
+  const u32x4 key = __builtin_nontemporal_load((const u32x4*)(k + from * kBytes));
+  const u32x4 value = __builtin_nontemporal_load((const u32x4*)(v + from * kBytes));
+  *(u32x4*)(k + to * kBytes) = key;
+  *(u32x4*)(v + to * kBytes) = value;
   if (E4M3 && piece == 0) {
     c.k_scale[to] = c.k_scale[from];
     c.v_scale[to] = c.v_scale[from];
   }
 }
 
+size_t align256(size_t x) { return (x + 255) / 256 * 256; }
+
+int chunks_of(const CacheParams& c) { return (c.capacity() + kChunk - 1) / kChunk; }
+
+struct Scratch {
+  size_t hist, list, counts, digits, bytes;
+  Scratch(const CacheParams& c, int batch) {
+    const size_t rows = (size_t)batch * c.hkv, chunks = rows * chunks_of(c);
+    hist = 0;
+    list = hist + chunks * 2 * kBins * 4;
+    counts = list + chunks * kChunk * 4;
+    digits = align256(counts + chunks * sizeof(ChunkCounts));
+    bytes = align256(digits + rows * sizeof(RowDigit));
+  }
+};
+
 }  // namespace
+
+size_t evict_scratch_bytes(const CacheParams& c, int batch) { return Scratch(c, batch).bytes; }
 
 hipError_t launch_evict(const CacheParams& c, bool e4m3, int batch, const int32_t* lens,
                         const float* weights, int budget, int recent, const int32_t* new_table,
                         int new_pages, int32_t* kept, int32_t* new_lens, float* new_weights,
-                        hipStream_t st) {
-  const int rows = batch * c.hkv;
-  auto* select = c.capacity() <= kSelWaves * kHeld * kStep ? evict_select<true>
-                                                           : evict_select<false>;
-  hipLaunchKernelGGL(select, dim3(rows), dim3(kSelThreads), 0, st, c, lens, weights, budget,
-                     recent, new_pages << c.shift, kept, new_lens, new_weights);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const int per = kMoveThreads / (e4m3 ? 8 : 16), chunks = (budget + per - 1) / per;
+                        void* scratch, hipStream_t st) {
+  const int rows = batch * c.hkv, chunks = chunks_of(c);
+  const Scratch s(c, batch);
+  char* at = (char*)scratch;
+  const EvictParams p{c,      lens, weights,  budget,      recent,
+                        chunks, new_pages << c.shift,        kept, new_lens, new_weights,
+                        (int*)(at + s.hist), (uint32_t*)(at + s.list),
+                        (ChunkCounts*)(at + s.counts), (RowDigit*)(at + s.digits)};
+  void (*const select[])(EvictParams) = {evict_count, evict_collect, evict_emit};
+  hipError_t e;
+  for (auto* kernel : select) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(rows * chunks)), dim3(kSelThreads), 0, st, p);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  const int per = kMoveThreads / (e4m3 ? 8 : 16), moves = (budget + per - 1) / per;
   auto* kernel = e4m3 ? evict_move<true> : evict_move<false>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((long long)rows * chunks)), dim3(kMoveThreads), 0, st,
-                     c, lens, budget, new_table, new_pages, kept);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((long long)rows * moves)), dim3(kMoveThreads), 0, st,
+                     c, lens, budget, moves, new_table, new_pages, kept);
   return hipGetLastError();
 }

@@ -143,6 +143,14 @@ int check_decode(const xattn_cache* cache, int batch, int hq, const int32_t* tab
   return XATTN_OK;
 }
 
+int check_evict(const xattn_cache* cache, const int32_t* table, int table_pages, int batch,
+                CacheParams* c) {
+  if (int rc = check_cache(cache, table, table_pages, batch, c)) return rc;
+  if ((long long)batch * cache->hkv * c->capacity() > (1ll << 31))
+    return fail(XATTN_ERR_UNSUPPORTED, "more than 2^31 cached vectors a batch");
+  return XATTN_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -223,13 +231,23 @@ int xattn_decode(const void* q, const xattn_cache* cache, int batch, int hq,
                   "xattn_decode");
 }
 
+int xattn_evict_workspace_size(const xattn_cache* cache, int batch, int table_pages,
+                               size_t* bytes) {
+  int rc;
+  CacheParams c;
+  if ((rc = check_evict(cache, nullptr, table_pages, batch, &c))) return rc;
+  if (!bytes) return fail(XATTN_ERR_ARG, "bytes is NULL");
+  *bytes = evict_scratch_bytes(c, batch);
+  return ok();
+}
+
 int xattn_cache_evict(const xattn_cache* cache, int batch, const int32_t* table, int table_pages,
                       const int32_t* lens, const float* weights, int budget, int recent,
                       const int32_t* new_table, int new_pages, int32_t* kept, int32_t* new_lens,
-                      float* new_weights, void* stream) {
+                      float* new_weights, void* workspace, size_t workspace_bytes, void* stream) {
   int rc;
   CacheParams c;
-  if ((rc = check_cache(cache, table, table_pages, batch, &c))) return rc;
+  if ((rc = check_evict(cache, table, table_pages, batch, &c))) return rc;
   if (budget < 1 || recent < 0 || recent > budget)
     return fail(XATTN_ERR_ARG, "1 <= budget and 0 <= recent <= budget (got %d, %d)", budget,
                 recent);
@@ -239,16 +257,20 @@ int xattn_cache_evict(const xattn_cache* cache, int batch, const int32_t* table,
       (long long)batch * c.hkv * ((budget + 15) / 16) > (1 << 23))
     return fail(XATTN_ERR_UNSUPPORTED, "more than 2^27 kept vectors a batch");
   if ((rc = check_cache_arrays(cache, table)) || (rc = check_pointer(lens, "lens", 4)) ||
-      (rc = check_pointer(weights, "weights", 4)) ||
+      (rc = check_pointer(weights, "weights", 16)) ||
       (rc = check_pointer(new_table, "new_table", 4)) || (rc = check_pointer(kept, "kept", 4)) ||
       (rc = check_pointer(new_lens, "new_lens", 4)) ||
       (rc = check_pointer(new_weights, "new_weights", 4)))
     return rc;
   if (new_lens == lens || new_weights == weights || new_table == table)
     return fail(XATTN_ERR_ARG, "an output is its own input, or new_table is table");
+  const size_t need = evict_scratch_bytes(c, batch);
+  if (!workspace || workspace_bytes < need || (uintptr_t)workspace % 16 != 0)
+    return fail(XATTN_ERR_WORKSPACE, "a 16-byte aligned workspace of %zu bytes needed, %zu given",
+                need, workspace ? workspace_bytes : (size_t)0);
   return launched(launch_evict(c, cache->type == XATTN_CACHE_E4M3, batch, lens, weights, budget,
                                recent, new_table, new_pages, kept, new_lens, new_weights,
-                               (hipStream_t)stream),
+                               workspace, (hipStream_t)stream),
                   "xattn_cache_evict");
 }
 

@@ -62,7 +62,8 @@ size_t decode_scratch_bytes(const xattn::CacheParams& c, int batch, int hq, bool
 hipError_t launch_decode(const void* q, const xattn::CacheParams& c, bool e4m3, int batch, int hq,
                          const int32_t* lens, void* o, float* lse, float* weights, void* scratch,
                          hipStream_t st);
+size_t evict_scratch_bytes(const xattn::CacheParams& c, int batch);
 hipError_t launch_evict(const xattn::CacheParams& c, bool e4m3, int batch, const int32_t* lens,
                         const float* weights, int budget, int recent, const int32_t* new_table,
                         int new_pages, int32_t* kept, int32_t* new_lens, float* new_weights,
-                        hipStream_t st);
+                        void* scratch, hipStream_t st);

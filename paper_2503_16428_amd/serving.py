@@ -286,8 +286,23 @@ def xattn_decode(q, cache: KVCache, table, lens, o=None, lse=None, weights=None,
     return o, lse
 
 
+@functools.lru_cache(maxsize=256)
+def _evict_bytes(hkv, page, batch, table_pages):
+    """Workspace bytes of a shape; a function of the shape alone."""
+    c = Cache(1, page, hkv, HEAD_DIM, 0, None, None, None, None)
+    n = ctypes.c_size_t(0)
+    _check(lib().xattn_evict_workspace_size(ctypes.byref(c), batch, table_pages, ctypes.byref(n)))
+    return n.value
+
+
+def evict_workspace_size(cache: KVCache, batch: int, table_pages: int) -> int:
+    """Bytes of xattn_cache_evict's workspace."""
+    _is_cache(cache)
+    return _evict_bytes(cache.hkv, cache.page, int(batch), int(table_pages))
+
+
 def xattn_cache_evict(cache: KVCache, table, lens, weights, new_table, budget: int, recent: int,
-                      kept=None, new_lens=None, new_weights=None, stream=None):
+                      kept=None, new_lens=None, new_weights=None, workspace=None, stream=None):
     """Moves the `budget` most valuable tokens of every sequence and key head (the last `recent`
     and the heaviest before them) to the pages of new_table, none of which is in table. Returns
     (kept int32 [batch, hkv, budget], new_lens int32 [batch], new_weights fp32 [batch, hkv,
@@ -307,9 +322,10 @@ def xattn_cache_evict(cache: KVCache, table, lens, weights, new_table, budget: i
     _is(kept, (b, h, budget), torch.int32, "kept")
     _is(new_lens, (b,), torch.int32, "new_lens")
     _is(new_weights, (b, h, new_width * cache.page), torch.float32, "new_weights")
-    tensors = (lens, weights, new_table, kept, new_lens, new_weights)
+    _check_workspace(workspace)
+    tensors = (lens, weights, new_table, kept, new_lens, new_weights, workspace)
     at = _here(table, (*tensors, cache.k), ("table", "lens", "weights", "new_table", "kept",
-                                            "new_lens", "new_weights", "cache"),
+                                            "new_lens", "new_weights", "workspace", "cache"),
                (table, *tensors))
     for n, out, given in (("new_lens", new_lens, lens), ("new_weights", new_weights, weights)):
         if out is not None and not _apart(out, given):
@@ -321,7 +337,11 @@ def xattn_cache_evict(cache: KVCache, table, lens, weights, new_table, budget: i
             new_lens = lens.new_empty((b,))
         if new_weights is None:
             new_weights = weights.new_empty((b, h, new_width * cache.page))
+        if workspace is None:
+            need = _evict_bytes(h, cache.page, b, width)
+            workspace = lens.new_empty((need,), dtype=torch.uint8)
     _check(lib().xattn_cache_evict(cache._ref, b, _ptr(table), width, _ptr(lens), _ptr(weights),
                                    budget, int(recent), _ptr(new_table), new_width, _ptr(kept),
-                                   _ptr(new_lens), _ptr(new_weights), _handle(stream, at)))
+                                   _ptr(new_lens), _ptr(new_weights), _ptr(workspace),
+                                   workspace.numel(), _handle(stream, at)))
     return kept, new_lens, new_weights

@@ -540,6 +540,20 @@ def test_evict_of_weights_alike():
         assert kept[0, 0].tolist() == list(range(1400)) + list(range(3901, 4001))
 
 
+@pytest.mark.parametrize("kind", ["spread", "alike", "one digit"])
+def test_evict_of_long_rows(kind):
+    """Rows of several workgroups: lengths around their borders, the last place in any of them."""
+    lens = [20001, 8193, 8192, 5001, 16384, 100]
+    g = gen(74)
+    w = torch.rand((6, 1, 20032), generator=g)
+    if kind == "alike":
+        w = (w * 8).floor()
+    elif kind == "one digit":  # weights whose upper 11 bits are the same
+        w = 1.0 + w * 2.0 ** -4
+    check_evict(w, lens, 64, 1, 5000, 37, kind == "alike")
+    check_evict(w, lens, 64, 1, 90, 0, False)
+
+
 def test_evict_with_missing_pages():
     w = torch.rand((2, 2, 128), generator=gen(73))
     check_evict(w, [120, 100], 16, 2, 50, 10, False, hole=(2, 1))

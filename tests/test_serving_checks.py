@@ -153,22 +153,33 @@ def test_decode_workspaces_grow_with_the_call():
 def evict(**kw):
     d = dict(cache=c_cache(), batch=1, table=FAKE, pages=2, lens=FAKE, weights=FAKE, budget=8,
              recent=2, new_table=FAKE + 64, new_pages=1, kept=FAKE, new_lens=FAKE + 64,
-             new_weights=FAKE + 64)
+             new_weights=FAKE + 64, ws=FAKE, bytes=1 << 40)
     d.update(kw)
     return X.lib().xattn_cache_evict(d["cache"], d["batch"], d["table"], d["pages"], d["lens"],
                                      d["weights"], d["budget"], d["recent"], d["new_table"],
                                      d["new_pages"], d["kept"], d["new_lens"], d["new_weights"],
-                                     None)
+                                     d["ws"], d["bytes"], None)
 
 
 @pytest.mark.parametrize("kw", [
     dict(table=None), dict(lens=None), dict(weights=None), dict(new_table=None), dict(kept=None),
     dict(new_lens=None), dict(new_weights=None), dict(budget=0), dict(recent=-1), dict(recent=9),
     dict(budget=17), dict(new_pages=0), dict(new_lens=FAKE), dict(new_weights=FAKE),
-    dict(new_table=FAKE), dict(batch=0), dict(weights=FAKE + 1), dict(cache=None),
+    dict(new_table=FAKE), dict(batch=0), dict(weights=FAKE + 68), dict(cache=None),
     *[dict(cache=c_cache(**c)) for c in BAD_CACHES]])
 def test_evict_refuses(kw):
     refused(evict(**kw))
+
+
+def test_evict_refuses_workspaces():
+    n = ctypes.c_size_t(0)
+    assert X.lib().xattn_evict_workspace_size(c_cache(), 1, 2, ctypes.byref(n)) == 0
+    for kw in (dict(ws=None), dict(bytes=n.value - 1), dict(ws=FAKE + 8)):
+        refused(evict(**kw), B.XATTN_ERR_WORKSPACE)
+    refused(X.lib().xattn_evict_workspace_size(c_cache(), 1, 2, None))
+    refused(X.lib().xattn_evict_workspace_size(c_cache(), 0, 2, ctypes.byref(n)))
+    expect("workspace must be", X.xattn_cache_evict, HostCache(), i32(3, 2), i32(3),
+           torch.zeros(3, 2, 32), i32(3, 1), 4, 1, workspace=torch.zeros(8))
 
 
 def test_evict_refuses_what_it_does_not_support():
