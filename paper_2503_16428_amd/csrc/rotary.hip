@@ -3,7 +3,11 @@
 //
 // Eight lanes share a vector of 128: lane j holds elements 8j .. 8j+7 and
 // 64+8j .. 64+8j+7 (two 16-byte loads), which are eight whole pairs in either
-// pairing. A thread computes its token's eight angles once and goes over heads.
+// pairing. A wave has eight tokens, the waves of a workgroup go over the heads in
+// turn: neighbouring heads of a token, which a projection leaves side by side, are
+// read together, and eight tokens of a head written together. A thread computes
+// its token's eight angles once, while its first vector is on the way, and loads
+// the next head's before it turns this one.
 #include "serve.h"
 
 using namespace xattn;
@@ -12,7 +16,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kLanes = 8;                   // lanes of a vector
-constexpr int kItems = kThreads / kLanes;   // tokens of a workgroup
+constexpr int kItems = kWave / kLanes;      // tokens of a workgroup
+constexpr int kWaves = kThreads / kWave;
 
 __device__ __forceinline__ float bf_lo(uint32_t w) {
   return __builtin_bit_cast(float, w << 16);
@@ -63,15 +68,18 @@ struct Angles {
 
 // Angles of a token's pairs: turns = pos * turn in fp64 (exact to 2^-52 of up
 // to 2^31 / 2 pi turns), of which the part of a turn goes to the hardware's sine
-// and cosine in fp32 (inputs in turns).
+// and cosine in fp32 (inputs in turns; off by at most 1.3e-7).
 template <bool IL>
 __device__ __forceinline__ Angles angles(const RotaryParams& p, const int32_t* pos,
                                          long long axis_stride, long long item, int j, float sign) {
+  double at[3];
+#pragma unroll
+  for (int x = 0; x < 3; ++x) at[x] = pos[min(x, p.axes - 1) * axis_stride + item];
   Angles a;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const int i = pair_of<IL>(j, e);
-    const double t = (double)pos[p.axis[i] * axis_stride + item] * p.turn[i];
+    const double t = (i < p.end[0] ? at[0] : i < p.end[1] ? at[1] : at[2]) * p.turn[i];
     const float f = (float)(t - __builtin_rint(t));
     a.c[e] = __builtin_amdgcn_cosf(f);
     a.s[e] = sign * __builtin_amdgcn_sinf(f);
@@ -90,34 +98,49 @@ __device__ __forceinline__ void rotate(Vec& v, const Angles& a, int n, int j) {
   }
 }
 
-__device__ __forceinline__ void store_bf16(uint16_t* p, const Vec& v) {
+// A lane's two pieces of a vector. Nothing here is read again before it has left
+// the caches.
+struct Raw {
+  u32x4 lo, hi;
+};
+__device__ __forceinline__ Raw load(const uint16_t* p) {
+  return Raw{__builtin_nontemporal_load((const u32x4*)p),
+             __builtin_nontemporal_load((const u32x4*)(p + 64))};
+}
+__device__ __forceinline__ void store(uint16_t* p, Raw r) {
+  __builtin_nontemporal_store(r.lo, (u32x4*)p);
+  __builtin_nontemporal_store(r.hi, (u32x4*)(p + 64));
+}
+__device__ __forceinline__ Raw pack(const Vec& v) {
   u32x4 lo, hi;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     lo[i] = pack_bf16(v.f[2 * i], v.f[2 * i + 1]);
     hi[i] = pack_bf16(v.f[8 + 2 * i], v.f[8 + 2 * i + 1]);
   }
-  *(u32x4*)p = lo;
-  *(u32x4*)(p + 64) = hi;
+  return Raw{lo, hi};
 }
 
 template <bool IL>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(
     const uint16_t* x, Strides xs, int tokens, long long items, int heads, int heads_per,
     const int32_t* __restrict__ pos, RotaryParams plan, float sign, uint16_t* out, Strides os) {
-  const int j = threadIdx.x % kLanes;
-  const long long item = (long long)blockIdx.x * kItems + threadIdx.x / kLanes;
-  if (item >= items) return;
+  const int lane = threadIdx.x % kWave, j = lane % kLanes;
+  const long long item = (long long)blockIdx.x * kItems + lane / kLanes;
+  int h = blockIdx.y * heads_per + threadIdx.x / kWave;
+  const int h1 = min((int)(blockIdx.y + 1) * heads_per, heads);
+  if (item >= items || h >= h1) return;
   const long long b = item / tokens, t = item - b * tokens;
-  const Angles a = angles<IL>(plan, pos, items, item, j, sign);
-  const int h0 = blockIdx.y * heads_per, h1 = min(h0 + heads_per, heads);
   x += b * xs.batch + t * xs.token + 8 * j;
   out += b * os.batch + t * os.token + 8 * j;
-  for (int h = h0; h < h1; ++h) {
-    const uint16_t* p = x + h * xs.head;
-    Vec v = unpack(*(const u32x4*)p, *(const u32x4*)(p + 64));
+  Raw next = load(x + h * xs.head);
+  const Angles a = angles<IL>(plan, pos, items, item, j, sign);
+  for (; h < h1; h += kWaves) {
+    const Raw now = next;
+    if (h + kWaves < h1) next = load(x + (h + kWaves) * xs.head);
+    Vec v = unpack(now.lo, now.hi);
     rotate<IL>(v, a, plan.n, j);
-    store_bf16(out + h * os.head, v);
+    store(out + h * os.head, pack(v));
   }
 }
 
@@ -189,33 +212,38 @@ __global__ __launch_bounds__(kThreads) void append_kernel(
     int tokens, long long items, int heads_per, const int32_t* __restrict__ count,
     const int32_t* __restrict__ start, const int32_t* __restrict__ pos, RotaryParams plan,
     CacheParams c) {
-  const int j = threadIdx.x % kLanes;
-  const long long item = (long long)blockIdx.x * kItems + threadIdx.x / kLanes;
-  if (item >= items) return;
+  const int lane = threadIdx.x % kWave, j = lane % kLanes;
+  const long long item = (long long)blockIdx.x * kItems + lane / kLanes;
+  int h = blockIdx.y * heads_per + threadIdx.x / kWave;
+  const int h1 = min((int)(blockIdx.y + 1) * heads_per, c.hkv);
+  if (item >= items || h >= h1) return;
   const long long b = item / tokens, t = item - b * tokens;
+  k += b * ks.batch + t * ks.token + 8 * j;
+  v += b * vs.batch + t * vs.token + 8 * j;
   if (count && t >= count[b]) return;
   const long long place = start[b] + t;
   const int column = page_column(place, c.shift, c.table_pages);
   if (column < 0) return;
+  Raw next_k = load(k + h * ks.head), next_v = load(v + h * vs.head);
   const int entry = c.table[b * c.table_pages + column];
   const int slot = (int)(place & ((1 << c.shift) - 1));
   if (page_row(entry, c.pages, c.hkv, 0, c.shift, slot) < 0) return;
   Angles a;
   if (ROT) a = angles<IL>(plan, pos, items, item, j, 1.f);
-  const int h0 = blockIdx.y * heads_per, h1 = min(h0 + heads_per, c.hkv);
-  k += b * ks.batch + t * ks.token + 8 * j;
-  v += b * vs.batch + t * vs.token + 8 * j;
-  for (int h = h0; h < h1; ++h) {
+  for (; h < h1; h += kWaves) {
     const long long row = page_row(entry, c.pages, c.hkv, h, c.shift, slot);
-    const uint16_t *kp = k + h * ks.head, *vp = v + h * vs.head;
-    const u32x4 k0 = *(const u32x4*)kp, k1 = *(const u32x4*)(kp + 64);
-    const u32x4 v0 = *(const u32x4*)vp, v1 = *(const u32x4*)(vp + 64);
+    Raw k_now = next_k;
+    const Raw v_now = next_v;
+    if (h + kWaves < h1) {
+      next_k = load(k + (h + kWaves) * ks.head);
+      next_v = load(v + (h + kWaves) * vs.head);
+    }
     if (E4M3) {
-      Vec key = unpack(k0, k1);
+      Vec key = unpack(k_now.lo, k_now.hi);
       const int ek = scale_exponent<IL, ROT>(key);
       if (ROT) rotate<IL>(key, a, plan.n, j);
       store_e4m3((uint8_t*)c.k + row * kHeadDim + 8 * j, key, ek);
-      const Vec value = unpack(v0, v1);
+      const Vec value = unpack(v_now.lo, v_now.hi);
       const int ev = scale_exponent<IL, false>(value);
       store_e4m3((uint8_t*)c.v + row * kHeadDim + 8 * j, value, ev);
       if (j == 0) {
@@ -223,27 +251,23 @@ __global__ __launch_bounds__(kThreads) void append_kernel(
         c.v_scale[row] = (uint8_t)(ev + 127);
       }
     } else {
-      uint16_t* to = (uint16_t*)c.k + row * kHeadDim + 8 * j;
       if (ROT) {
-        Vec key = unpack(k0, k1);
+        Vec key = unpack(k_now.lo, k_now.hi);
         rotate<IL>(key, a, plan.n, j);
-        store_bf16(to, key);
-      } else {
-        *(u32x4*)to = k0;
-        *(u32x4*)(to + 64) = k1;
+        k_now = pack(key);
       }
-      to = (uint16_t*)c.v + row * kHeadDim + 8 * j;
-      *(u32x4*)to = v0;
-      *(u32x4*)(to + 64) = v1;
+      store((uint16_t*)c.k + row * kHeadDim + 8 * j, k_now);
+      store((uint16_t*)c.v + row * kHeadDim + 8 * j, v_now);
     }
   }
 }
 
-// Heads that a thread goes over: as many as leave eight workgroups a CU.
-int heads_per_thread(long long groups, int heads) {
-  const long long want = 8 * 256;
-  long long per = groups * heads / want;
-  return (int)(per < 1 ? 1 : per > heads ? heads : per);
+// Heads of a workgroup: as many as leave 32 workgroups a CU, four at least (8
+// a CU: 32K tokens of 32 heads 104.9 -> 101.0 us, others alike).
+constexpr long long kWant = 32 * 256;
+int heads_per_group(long long groups, int heads) {
+  const long long per = (groups * heads / kWant + kWaves - 1) / kWaves * kWaves;
+  return (int)(per < kWaves ? kWaves : per > heads ? heads : per);
 }
 
 }  // namespace
@@ -252,7 +276,7 @@ hipError_t launch_rotary(const void* x, const Strides& xs, int batch, int heads,
                          const int32_t* pos, const RotaryParams& plan, bool interleaved,
                          bool inverse, void* out, const Strides& os, hipStream_t st) {
   const long long items = (long long)batch * tokens, groups = (items + kItems - 1) / kItems;
-  const int per = heads_per_thread(groups, heads);
+  const int per = heads_per_group(groups, heads);
   const dim3 grid((unsigned)groups, (heads + per - 1) / per);
   auto* kernel = interleaved ? rotary_kernel<true> : rotary_kernel<false>;
   hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, st, (const uint16_t*)x, xs, tokens, items,
@@ -265,7 +289,7 @@ hipError_t launch_append(const void* k, const Strides& ks, const void* v, const 
                          const int32_t* pos, const RotaryParams* plan, bool interleaved,
                          const CacheParams& c, bool e4m3, hipStream_t st) {
   const long long items = (long long)batch * tokens, groups = (items + kItems - 1) / kItems;
-  const int per = heads_per_thread(groups, c.hkv);
+  const int per = heads_per_group(groups, c.hkv);
   const dim3 grid((unsigned)groups, (c.hkv + per - 1) / per);
   auto* kernel = plan ? (interleaved ? (e4m3 ? append_kernel<true, true, true>
                                              : append_kernel<true, true, false>)

@@ -74,9 +74,10 @@ int check_plan(const xattn_rotary_plan* plan, RotaryParams* out) {
     for (int i = 0; i < pairs; ++i, ++n) {
       if (!std::isfinite(plan->freq[n])) return fail(XATTN_ERR_ARG, "freq[%d] is not finite", n);
       out->turn[n] = plan->freq[n] / kTwoPi;
-      out->axis[n] = (unsigned char)a;
     }
+    if (a < 2) out->end[a] = n;
   }
+  out->axes = plan->axes;
   out->n = n;
   return XATTN_OK;
 }

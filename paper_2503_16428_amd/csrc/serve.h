@@ -31,12 +31,11 @@ struct Strides {
   long long batch, head, token;
 };
 
-// A plan as the kernels take it (by value): turns per position of each pair,
-// its axis, and how many pairs are rotated.
+// A plan as the kernels take it (by value): turns per position of each pair, the
+// first pairs behind axes 0 and 1, and how many pairs are rotated.
 struct RotaryParams {
   double turn[64];
-  unsigned char axis[64];
-  int n;
+  int axes, end[2], n;
 };
 
 // The cache and one batch's page table (by value).
