@@ -118,15 +118,23 @@ struct PieceOf<true> {
   typedef u32x2 type;
 };
 
-// Workgroups that share a batch's units: three a CU, as many as are resident.
+// Workgroups that share a batch's units: two a CU, or three, as many as are
+// resident, where rows are many and a workgroup often begins a new one, which the
+// others of its CU then make up for. In us, two / three a CU, 8 key heads: one
+// sequence of 128K 88 / 92, 4 of 32K 88 / 91, 48 of up to 8000 133 / 138, in 8 bits
+// 72 / 78; 64 of up to 8000 183 / 177, 100 / 95, of up to 2000 63 / 59, 44 / 39;
+// 64 of 2048, a row each, 88 / 96. (Any number that is no multiple of the CUs
+// gives some of them more work: 384, 103 us at 128K.)
 constexpr int kMostWorkers = 768;
+inline int most_workers(int rows) { return rows >= 512 ? kMostWorkers : 512; }
 
 // How `units` are shared out: the first `more` workgroups have per + 1 of them,
-// the others per; no more workgroups than units.
+// the others per; no more workgroups than half the units (one key head, 64K: 20.4
+// -> 16.8 us for the fewer parts to join).
 struct Shares {
   int workers, per, more;
   __device__ Shares(int units, int most) {
-    workers = units < most ? units : most;
+    workers = min((units + 1) / 2, most);
     per = workers ? units / workers : 0;
     more = units - workers * per;
   }
@@ -275,6 +283,8 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(Decod
         if (E4M3) k_scale[i] = *(const uint32_t*)(p.c.k_scale + r + 4u * g);
       }
     };
+    // Values pass the caches by: 7 % faster. (Keys, of which a load has halves of
+    // lines, are slower that way; brought to LDS in whole lines they are as fast.)
     auto load_v = [&](const char* a, int i, int y) {
       v[i][y] = __builtin_nontemporal_load((const Piece*)(a + (E4M3 ? 128 : 256) * y + v_off));
     };
@@ -683,10 +693,11 @@ hipError_t launch_decode(const void* q, const CacheParams& c, bool e4m3, int bat
   p.ml = (float*)((char*)scratch + s.ml);
   p.stat = weights ? (float*)((char*)scratch + s.stat) : nullptr;
   p.z = weights ? (float*)((char*)scratch + s.z) : nullptr;
-  // no more workgroups than there can be units
-  const long long most = (long long)batch * c.hkv * p.row_tiles *
-                         ((c.capacity() + kUnit - 1) / kUnit);
-  p.most_workers = most < kMostWorkers ? (int)most : kMostWorkers;
+  // no more workgroups than there can be shares
+  const int rows = batch * c.hkv * p.row_tiles;
+  const long long units = (long long)rows * ((c.capacity() + kUnit - 1) / kUnit);
+  p.most_workers = most_workers(rows);
+  if ((units + 1) / 2 < p.most_workers) p.most_workers = (int)((units + 1) / 2);
   auto* kernel = p.tile_rows <= kRows ? (e4m3 ? decode_kernel<true, 1> : decode_kernel<false, 1>)
                                       : (e4m3 ? decode_kernel<true, 2> : decode_kernel<false, 2>);
   hipLaunchKernelGGL(kernel, dim3(p.most_workers), dim3(kThreads), 0, st, p);

@@ -141,6 +141,10 @@ int check_decode(const xattn_cache* cache, int batch, int hq, const int32_t* tab
   if ((long long)batch * hq > (1 << 20) ||
       (long long)batch * cache->hkv * ((c->capacity() + 255) / 256) > (1 << 23))
     return fail(XATTN_ERR_UNSUPPORTED, "more than 2^20 query heads or 2^31 cached vectors a batch");
+  // units of 128 keys of every row of up to 32 heads, in 32 bits
+  const long long tiles = (hq / cache->hkv + 31) / 32;
+  if (batch * cache->hkv * tiles * ((c->capacity() + 127) / 128) > (1 << 30))
+    return fail(XATTN_ERR_UNSUPPORTED, "more than 2^30 units of 128 keys and 32 heads a batch");
   return XATTN_OK;
 }
 
