@@ -4,10 +4,14 @@
 // Eight lanes share a vector of 128: lane j holds elements 8j .. 8j+7 and
 // 64+8j .. 64+8j+7 (two 16-byte loads), which are eight whole pairs in either
 // pairing. A wave has eight tokens, the waves of a workgroup go over the heads in
-// turn: neighbouring heads of a token, which a projection leaves side by side, are
-// read together, and eight tokens of a head written together. A thread computes
+// turn (two or one of them where there are no more heads, the others then have
+// other tokens): neighbouring heads of a token, which a projection leaves side by
+// side, are read together, and eight tokens of a head written together. A thread
+// computes
 // its token's eight angles once, while its first vector is on the way, and loads
 // the next head's before it turns this one.
+#include <type_traits>
+
 #include "serve.h"
 
 using namespace xattn;
@@ -16,8 +20,25 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kLanes = 8;                   // lanes of a vector
-constexpr int kItems = kWave / kLanes;      // tokens of a workgroup
+constexpr int kItems = kWave / kLanes;      // tokens of a wave
 constexpr int kWaves = kThreads / kWave;
+
+// A launch: how many waves share out the heads, and how many heads a workgroup has.
+struct Split {
+  int waves, heads;
+};
+// A thread's token, and its first head and the one behind its last.
+struct Place {
+  long long item;
+  int h, h1;
+  __device__ Place(Split s, int heads) {
+    const int wave = threadIdx.x / kWave;
+    item = (long long)blockIdx.x * (kItems * (kWaves / s.waves)) + wave / s.waves * kItems +
+           threadIdx.x % kWave / kLanes;
+    h = blockIdx.y * s.heads + wave % s.waves;
+    h1 = min((int)(blockIdx.y + 1) * s.heads, heads);
+  }
+};
 
 __device__ __forceinline__ float bf_lo(uint32_t w) {
   return __builtin_bit_cast(float, w << 16);
@@ -62,39 +83,98 @@ __device__ __forceinline__ int pair_of(int j, int e) {
   return IL ? (e < 4 ? 4 * j + e : 32 + 4 * j + e - 4) : 8 * j + e;
 }
 
+template <class T>
 struct Angles {
-  float c[8], s[8];
+  T c[8], s[8];
 };
 
-// Angles of a token's pairs: turns = pos * turn in fp64 (exact to 2^-52 of up
-// to 2^31 / 2 pi turns), of which the part of a turn goes to the hardware's sine
-// and cosine in fp32 (inputs in turns; off by at most 1.3e-7).
-template <bool IL>
-__device__ __forceinline__ Angles angles(const RotaryParams& p, const int32_t* pos,
-                                         long long axis_stride, long long item, int j, float sign) {
+// Sine and cosine of a part of a turn, |t| <= 1/2: of the quarter turn next to it
+// and the rest, |x| <= pi / 4, by their series to x^13 and x^12 (off by x^14 / 14!,
+// at most 4e-13).
+__device__ __forceinline__ void sin_cos(double t, double* s, double* c) {
+  const double q = __builtin_rint(4.0 * t);
+  const double x = 6.283185307179586476925 * (t - 0.25 * q), y = x * x;
+  const double sine =
+      x + x * y * (-1.0 / 6 + y * (1.0 / 120 + y * (-1.0 / 5040 + y * (1.0 / 362880 +
+          y * (-1.0 / 39916800 + y * (1.0 / 6227020800))))));
+  const double cosine =
+      1.0 + y * (-1.0 / 2 + y * (1.0 / 24 + y * (-1.0 / 720 + y * (1.0 / 40320 +
+          y * (-1.0 / 3628800 + y * (1.0 / 479001600))))));
+  const int n = (int)q & 3;
+  const double a = n & 1 ? cosine : sine, b = n & 1 ? sine : cosine;
+  *s = n & 2 ? -a : a;
+  *c = n == 1 || n == 2 ? -b : b;
+}
+// In fp32 the hardware's, which take turns (off by at most 1.3e-7).
+__device__ __forceinline__ void sin_cos(float t, float* s, float* c) {
+  *s = __builtin_amdgcn_sinf(t);
+  *c = __builtin_amdgcn_cosf(t);
+}
+
+// The positions of a token, and the part of a turn of its pair i: turns = pos *
+// turn in fp64, exact to 2^-52 of up to 2^31 / 2 pi of them.
+struct Position {
   double at[3];
+  __device__ Position(const RotaryParams& p, const int32_t* pos, long long axis_stride,
+                      long long item) {
 #pragma unroll
-  for (int x = 0; x < 3; ++x) at[x] = pos[min(x, p.axes - 1) * axis_stride + item];
-  Angles a;
+    for (int x = 0; x < 3; ++x) at[x] = pos[min(x, p.axes - 1) * axis_stride + item];
+  }
+  __device__ double turn(const RotaryParams& p, int i) const {
+    const double t = (i < p.end[0] ? at[0] : i < p.end[1] ? at[1] : at[2]) * p.turn[i];
+    return t - __builtin_rint(t);
+  }
+};
+
+// Angles of a lane's pairs of a token.
+template <bool IL>
+__device__ __forceinline__ Angles<float> angles(const RotaryParams& p, const int32_t* pos,
+                                                long long axis_stride, long long item, int j,
+                                                float sign) {
+  const Position at(p, pos, axis_stride, item);
+  Angles<float> a;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const int i = pair_of<IL>(j, e);
-    const double t = (i < p.end[0] ? at[0] : i < p.end[1] ? at[1] : at[2]) * p.turn[i];
-    const float f = (float)(t - __builtin_rint(t));
-    a.c[e] = __builtin_amdgcn_cosf(f);
-    a.s[e] = sign * __builtin_amdgcn_sinf(f);
+    sin_cos((float)at.turn(p, pair_of<IL>(j, e)), &a.s[e], &a.c[e]);
+    a.s[e] *= sign;
   }
   return a;
 }
 
-template <bool IL>
-__device__ __forceinline__ void rotate(Vec& v, const Angles& a, int n, int j) {
+// The same in fp64, of the workgroup's tokens, each pair by one thread.
+struct SharedAngles {
+  double2 sc[kItems * kWaves][64 + 1];  // sine, cosine
+  __device__ void compute(const RotaryParams& p, const int32_t* pos, long long items, Split s) {
+    const int per = kLanes * s.waves;  // threads of a token
+    const int token = threadIdx.x / per;
+    const long long item = (long long)blockIdx.x * (kThreads / per) + token;
+    if (item < items) {
+      const Position at(p, pos, items, item);
+      for (int i = threadIdx.x % per; i < 64; i += per)
+        sin_cos(at.turn(p, i), &sc[token][i].x, &sc[token][i].y);
+    }
+    __syncthreads();
+  }
+  template <bool IL>
+  __device__ Angles<double> of(int token, int j) const {
+    Angles<double> a;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      a.s[e] = sc[token][pair_of<IL>(j, e)].x;
+      a.c[e] = sc[token][pair_of<IL>(j, e)].y;
+    }
+    return a;
+  }
+};
+
+template <bool IL, class T>
+__device__ __forceinline__ void rotate(Vec& v, const Angles<T>& a, int n, int j) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float x = v.f[first_of<IL>(e)], y = v.f[second_of<IL>(e)];
     const bool turned = pair_of<IL>(j, e) < n;
-    v.f[first_of<IL>(e)] = turned ? x * a.c[e] - y * a.s[e] : x;
-    v.f[second_of<IL>(e)] = turned ? x * a.s[e] + y * a.c[e] : y;
+    v.f[first_of<IL>(e)] = turned ? (float)(x * a.c[e] - y * a.s[e]) : x;
+    v.f[second_of<IL>(e)] = turned ? (float)(x * a.s[e] + y * a.c[e]) : y;
   }
 }
 
@@ -123,21 +203,22 @@ __device__ __forceinline__ Raw pack(const Vec& v) {
 
 template <bool IL>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(
-    const uint16_t* x, Strides xs, int tokens, long long items, int heads, int heads_per,
+    const uint16_t* x, Strides xs, int tokens, long long items, int heads, Split split,
     const int32_t* __restrict__ pos, RotaryParams plan, float sign, uint16_t* out, Strides os) {
-  const int lane = threadIdx.x % kWave, j = lane % kLanes;
-  const long long item = (long long)blockIdx.x * kItems + lane / kLanes;
-  int h = blockIdx.y * heads_per + threadIdx.x / kWave;
-  const int h1 = min((int)(blockIdx.y + 1) * heads_per, heads);
+  const int j = threadIdx.x % kLanes;
+  const Place place(split, heads);
+  const long long item = place.item;
+  const int h1 = place.h1, step = split.waves;
+  int h = place.h;
   if (item >= items || h >= h1) return;
   const long long b = item / tokens, t = item - b * tokens;
   x += b * xs.batch + t * xs.token + 8 * j;
   out += b * os.batch + t * os.token + 8 * j;
   Raw next = load(x + h * xs.head);
-  const Angles a = angles<IL>(plan, pos, items, item, j, sign);
-  for (; h < h1; h += kWaves) {
+  const Angles<float> a = angles<IL>(plan, pos, items, item, j, sign);
+  for (; h < h1; h += step) {
     const Raw now = next;
-    if (h + kWaves < h1) next = load(x + (h + kWaves) * xs.head);
+    if (h + step < h1) next = load(x + (h + step) * xs.head);
     Vec v = unpack(now.lo, now.hi);
     rotate<IL>(v, a, plan.n, j);
     store(out + h * os.head, pack(v));
@@ -209,13 +290,18 @@ __device__ __forceinline__ void store_e4m3(uint8_t* p, const Vec& v, int e) {
 template <bool IL, bool ROT, bool E4M3>
 __global__ __launch_bounds__(kThreads) void append_kernel(
     const uint16_t* __restrict__ k, Strides ks, const uint16_t* __restrict__ v, Strides vs,
-    int tokens, long long items, int heads_per, const int32_t* __restrict__ count,
+    int tokens, long long items, Split split, const int32_t* __restrict__ count,
     const int32_t* __restrict__ start, const int32_t* __restrict__ pos, RotaryParams plan,
     CacheParams c) {
-  const int lane = threadIdx.x % kWave, j = lane % kLanes;
-  const long long item = (long long)blockIdx.x * kItems + lane / kLanes;
-  int h = blockIdx.y * heads_per + threadIdx.x / kWave;
-  const int h1 = min((int)(blockIdx.y + 1) * heads_per, c.hkv);
+  // A key that goes to 8 bits is turned in fp64: a value that rounds the other way
+  // is off by a sixteenth.
+  __shared__ typename std::conditional<ROT && E4M3, SharedAngles, int>::type shared;
+  if constexpr (ROT && E4M3) shared.compute(plan, pos, items, split);
+  const int j = threadIdx.x % kLanes;
+  const Place at(split, c.hkv);
+  const long long item = at.item;
+  const int h1 = at.h1, step = split.waves;
+  int h = at.h;
   if (item >= items || h >= h1) return;
   const long long b = item / tokens, t = item - b * tokens;
   k += b * ks.batch + t * ks.token + 8 * j;
@@ -228,20 +314,22 @@ __global__ __launch_bounds__(kThreads) void append_kernel(
   const int entry = c.table[b * c.table_pages + column];
   const int slot = (int)(place & ((1 << c.shift) - 1));
   if (page_row(entry, c.pages, c.hkv, 0, c.shift, slot) < 0) return;
-  Angles a;
-  if (ROT) a = angles<IL>(plan, pos, items, item, j, 1.f);
-  for (; h < h1; h += kWaves) {
+  Angles<float> a;
+  Angles<double> exact;
+  if (ROT && !E4M3) a = angles<IL>(plan, pos, items, item, j, 1.f);
+  if constexpr (ROT && E4M3) exact = shared.template of<IL>((int)(item - (long long)blockIdx.x * (kItems * (kWaves / step))), j);
+  for (; h < h1; h += step) {
     const long long row = page_row(entry, c.pages, c.hkv, h, c.shift, slot);
     Raw k_now = next_k;
     const Raw v_now = next_v;
-    if (h + kWaves < h1) {
-      next_k = load(k + (h + kWaves) * ks.head);
-      next_v = load(v + (h + kWaves) * vs.head);
+    if (h + step < h1) {
+      next_k = load(k + (h + step) * ks.head);
+      next_v = load(v + (h + step) * vs.head);
     }
     if (E4M3) {
       Vec key = unpack(k_now.lo, k_now.hi);
       const int ek = scale_exponent<IL, ROT>(key);
-      if (ROT) rotate<IL>(key, a, plan.n, j);
+      if (ROT) rotate<IL>(key, exact, plan.n, j);
       store_e4m3((uint8_t*)c.k + row * kHeadDim + 8 * j, key, ek);
       const Vec value = unpack(v_now.lo, v_now.hi);
       const int ev = scale_exponent<IL, false>(value);
@@ -262,12 +350,19 @@ __global__ __launch_bounds__(kThreads) void append_kernel(
   }
 }
 
-// Heads of a workgroup: as many as leave 32 workgroups a CU, four at least (8
-// a CU: 32K tokens of 32 heads 104.9 -> 101.0 us, others alike).
+// Workgroups that are to be left when their heads are made more: 32 a CU (8: 32K
+// tokens of 32 heads 104.9 -> 101.0 us the other way, others alike).
 constexpr long long kWant = 32 * 256;
-int heads_per_group(long long groups, int heads) {
-  const long long per = (groups * heads / kWant + kWaves - 1) / kWaves * kWaves;
-  return (int)(per < kWaves ? kWaves : per > heads ? heads : per);
+
+Split split_of(long long items, int heads, dim3* grid) {
+  Split s;
+  s.waves = heads >= kWaves ? kWaves : heads >= 2 ? 2 : 1;
+  const int tokens = kItems * (kWaves / s.waves);
+  const long long groups = (items + tokens - 1) / tokens;
+  const long long per = (groups * heads / kWant + s.waves - 1) / s.waves * s.waves;
+  s.heads = (int)(per < s.waves ? s.waves : per > heads ? heads : per);
+  *grid = dim3((unsigned)groups, (heads + s.heads - 1) / s.heads);
+  return s;
 }
 
 }  // namespace
@@ -275,12 +370,12 @@ int heads_per_group(long long groups, int heads) {
 hipError_t launch_rotary(const void* x, const Strides& xs, int batch, int heads, int tokens,
                          const int32_t* pos, const RotaryParams& plan, bool interleaved,
                          bool inverse, void* out, const Strides& os, hipStream_t st) {
-  const long long items = (long long)batch * tokens, groups = (items + kItems - 1) / kItems;
-  const int per = heads_per_group(groups, heads);
-  const dim3 grid((unsigned)groups, (heads + per - 1) / per);
+  const long long items = (long long)batch * tokens;
+  dim3 grid;
+  const Split split = split_of(items, heads, &grid);
   auto* kernel = interleaved ? rotary_kernel<true> : rotary_kernel<false>;
   hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, st, (const uint16_t*)x, xs, tokens, items,
-                     heads, per, pos, plan, inverse ? -1.f : 1.f, (uint16_t*)out, os);
+                     heads, split, pos, plan, inverse ? -1.f : 1.f, (uint16_t*)out, os);
   return hipGetLastError();
 }
 
@@ -288,9 +383,9 @@ hipError_t launch_append(const void* k, const Strides& ks, const void* v, const 
                          int batch, int tokens, const int32_t* count, const int32_t* start,
                          const int32_t* pos, const RotaryParams* plan, bool interleaved,
                          const CacheParams& c, bool e4m3, hipStream_t st) {
-  const long long items = (long long)batch * tokens, groups = (items + kItems - 1) / kItems;
-  const int per = heads_per_group(groups, c.hkv);
-  const dim3 grid((unsigned)groups, (c.hkv + per - 1) / per);
+  const long long items = (long long)batch * tokens;
+  dim3 grid;
+  const Split split = split_of(items, c.hkv, &grid);
   auto* kernel = plan ? (interleaved ? (e4m3 ? append_kernel<true, true, true>
                                              : append_kernel<true, true, false>)
                                      : (e4m3 ? append_kernel<false, true, true>
@@ -298,7 +393,7 @@ hipError_t launch_append(const void* k, const Strides& ks, const void* v, const 
                       : (e4m3 ? append_kernel<false, false, true>
                               : append_kernel<false, false, false>);
   hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, st, (const uint16_t*)k, ks,
-                     (const uint16_t*)v, vs, tokens, items, per, count, start, pos,
+                     (const uint16_t*)v, vs, tokens, items, split, count, start, pos,
                      plan ? *plan : RotaryParams{}, c);
   return hipGetLastError();
 }

@@ -86,8 +86,8 @@ int check_tokens(int batch, int heads, int tokens) {
   if (batch < 1 || heads < 1 || tokens < 1)
     return fail(XATTN_ERR_ARG, "sizes must be positive (batch=%d heads=%d tokens=%d)", batch, heads,
                 tokens);
-  if ((long long)batch * tokens > (1ll << 28) || heads > 65535)
-    return fail(XATTN_ERR_UNSUPPORTED, "more than 2^28 tokens or 65535 heads");
+  if ((long long)batch * tokens > (1ll << 26) || heads > 65535)
+    return fail(XATTN_ERR_UNSUPPORTED, "more than 2^26 tokens or 65535 heads");
   return XATTN_OK;
 }
 
