@@ -405,7 +405,9 @@ int xattn_cache_append(const void *k, const int64_t *k_strides, const void *v,
  *   lse[b][h] = log sum_t exp(q[b][h] . k_t / sqrt(128))      (natural log)
  * with the head's keys and values (contiguous GQA grouping, any group size).
  * The new token's own key is one of the cached ones: append first. Rows without
- * a key get o = 0 and lse = -inf; keys whose products are -inf have no weight.
+ * a key get o = 0 and lse = -inf; keys whose products are -inf have no weight
+ * (their values must be finite, as every value with a weight of 0 must). What a
+ * page holds behind the last token has no effect, whatever it is.
  * Several new tokens of one sequence are several rows with the same pages and
  * each its own length.
  *   q        bf16 [batch][hq][128]; o the same (output)
@@ -415,10 +417,11 @@ int xattn_cache_append(const void *k, const int64_t *k_strides, const void *v,
  *            a key head grows by the sum of its query heads' softmax_t, for
  *            t < lens[b]; what lies behind is left as it was
  *   workspace  at least xattn_decode_workspace_size() bytes (`weights`: whether
- *            the call has them); its contents on entry are ignored
- * QK^T is bf16 on the matrix cores (e4m3 keys are exact in bf16) with fp32
- * accumulation; the softmax, P and the PV product are fp32, the output rounded
- * once.
+ *            the call has them), 16-byte aligned; its contents on entry are
+ *            ignored. Calls that may run at the same time need one each.
+ * QK^T and PV run on the bf16 matrix cores with fp32 accumulation (e4m3 values
+ * are exact in bf16); the softmax is fp32, and P goes into PV as the sum of two
+ * bf16 values, within 2^-16 of it. The output is rounded once.
  */
 int xattn_decode_workspace_size(const xattn_cache *cache, int batch, int hq, int table_pages,
                                 int weights, size_t *bytes);
@@ -445,8 +448,7 @@ int xattn_decode(const void *q, const xattn_cache *cache, int batch, int hq,
  *   new_lens     int32 [batch] (output): min(lens, budget); must not be lens
  *   new_weights  fp32 [batch][hkv][new_pages * page] (output): the kept tokens'
  *                weights, 0 behind them; no memory of weights
- *   workspace    at least xattn_evict_workspace_size() bytes; its contents on entry
- *                are ignored
+ *   workspace    as for xattn_decode, xattn_evict_workspace_size() bytes
  * The weights are 16-byte aligned. 1 <= budget, 0 <= recent <= budget. Page rows behind the kept tokens are left
  * as they were.
  */

@@ -182,7 +182,11 @@ def _allocating(stream):
 
 
 def _handle(stream, at):
-    return torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(at)
+    if stream.device_index != at:
+        _fail(f"stream must be one of the current device {at}, got {stream.device}")
+    return stream.cuda_stream
 
 
 def xattn_rotary(x, pos, rotary: Rotary, inverse=False, out=None, stream=None):

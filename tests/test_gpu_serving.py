@@ -457,6 +457,78 @@ def test_decode_is_deterministic_and_follows_its_stream():
         assert torch.equal(w2, w)
 
 
+def test_two_calls_at_once():
+    """Different batches on two streams, each with its own workspace: the results of each alone."""
+    cases = []
+    for i, (lens, e4m3) in enumerate((([3000, 10, 777], False), ([2500, 2500], True))):
+        q, k, v, s, table = decode_case(len(lens), 8, 2, 64, lens, e4m3, seed=200 + i)
+        w = torch.rand((len(lens), 2, table.shape[1] * 64), generator=gen(210 + i))
+        cases.append((q.cuda(), on_gpu(k, v, s), table.cuda(), ints(lens), w))
+    alone = []
+    for q, cache, table, lens, w in cases:
+        u = w.cuda()
+        alone.append((*X.xattn_decode(q, cache, table, lens, weights=u, want_lse=True), u))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    held = [w.cuda() for *_, w in cases]
+    torch.cuda.synchronize()
+    outs = [X.xattn_decode(q, cache, table, lens, weights=u, want_lse=True, stream=st)
+            for (q, cache, table, lens, _), u, st in zip(cases, held, streams)]
+    torch.cuda.synchronize()
+    for (o, lse, w), (o2, lse2), w2 in zip(alone, outs, held):
+        assert torch.equal(bits(o), bits(o2)) and torch.equal(lse, lse2) and torch.equal(w, w2)
+
+
+def test_scales_far_apart():
+    """Values of one vector are alike in size, those of different tokens 2^60 apart."""
+    lens = [130, 33]
+    q, k, v, s, table = decode_case(2, 6, 2, 16, lens, True)
+    g = gen(220)
+    ks = s[0].clone()
+    ks[torch.rand(ks.shape, generator=g) < 0.5] -= 40  # products of next to nothing
+    vs = (s[1].int() + torch.randint(-30, 31, s[1].shape, generator=g)).to(torch.uint8)
+    check_decode(q, k, v, (ks, vs), table, lens)
+
+
+def test_workspaces_may_hold_anything():
+    lens = [900, 0, 77, 2000]
+    q, k, v, s, table = decode_case(4, 20, 1, 32, lens, False)
+    cache, qd, td, ld = on_gpu(k, v, s), q.cuda(), table.cuda(), ints(lens)
+    w0 = torch.rand((4, 1, table.shape[1] * 32), generator=gen(230)).cuda()
+    new_table = torch.zeros((4, 8), dtype=torch.int32, device="cuda") - 1  # nothing is moved
+    want = None
+    for fill in (0, 255, 127, 1):
+        ws = torch.full((X.decode_workspace_size(cache, 4, 20, table.shape[1], True),), fill,
+                        dtype=torch.uint8, device="cuda")
+        es = torch.full((X.evict_workspace_size(cache, 4, table.shape[1]),), fill,
+                        dtype=torch.uint8, device="cuda")
+        w = w0.clone()
+        got = (*X.xattn_decode(qd, cache, td, ld, weights=w, want_lse=True, workspace=ws), w,
+               *X.xattn_cache_evict(cache, td, ld, w0, new_table, 200, 7, workspace=es))
+        want = want or got
+        assert all(torch.equal(bits(a), bits(b)) for a, b in zip(got, want)), fill
+
+
+def test_projections_are_read_where_they_are():
+    """q, k and v as slices of one projection's output [batch, tokens, heads, 128]."""
+    qkv = normal((2, 9, 8 + 2 + 2, 128), 240).cuda()
+    q, k, v = (t.transpose(1, 2) for t in qkv.split([8, 2, 2], dim=2))
+    pos = torch.arange(9, dtype=torch.int32).expand(1, 2, 9).contiguous().cuda()
+    plan = X.Rotary([64], R.freqs([64]))
+    assert torch.equal(bits(X.xattn_rotary(q, pos, plan)),
+                       bits(X.xattn_rotary(q.contiguous(), pos, plan)))
+    one, two = pool(3, 2, 16, False), pool(3, 2, 16, False)
+    table, start = ints([[0], [2]]), ints([0, 7])
+    X.xattn_cache_append(k, v, one, table, start, pos=pos, rotary=plan)
+    X.xattn_cache_append(k.contiguous(), v.contiguous(), two, table, start, pos=pos, rotary=plan)
+    assert all(torch.equal(a, b) for a, b in zip(arrays(one), arrays(two)))
+    before = qkv.clone()
+    X.xattn_rotary(q, pos, plan, out=q)  # in place, the keys and values beside it untouched
+    assert torch.equal(bits(qkv[:, :, 8:]), bits(before[:, :, 8:]))
+    with pytest.raises(X.XAttnError):
+        X.xattn_rotary(q, pos, plan, out=qkv.view(-1)[:q.numel()].view(q.shape))
+
+
 def test_decode_offsets_past_32_bits():
     """A pool of more than 2^31 values: its last pages hold the sequence."""
     page, hkv = 256, 8
