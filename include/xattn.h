@@ -448,7 +448,8 @@ int xattn_decode(const void *q, const xattn_cache *cache, int batch, int hq,
  *   new_lens     int32 [batch] (output): min(lens, budget); must not be lens
  *   new_weights  fp32 [batch][hkv][new_pages * page] (output): the kept tokens'
  *                weights, 0 behind them; no memory of weights
- *   workspace    as for xattn_decode, xattn_evict_workspace_size() bytes
+ *   workspace    as for xattn_decode, xattn_evict_workspace_size() bytes (0 for
+ *                rows of up to 16384 tokens, then it may be NULL)
  * The weights are 16-byte aligned. 1 <= budget, 0 <= recent <= budget. Page rows behind the kept tokens are left
  * as they were.
  */

@@ -270,7 +270,7 @@ int xattn_cache_evict(const xattn_cache* cache, int batch, const int32_t* table,
   if (new_lens == lens || new_weights == weights || new_table == table)
     return fail(XATTN_ERR_ARG, "an output is its own input, or new_table is table");
   const size_t need = evict_scratch_bytes(c, batch);
-  if (!workspace || workspace_bytes < need || (uintptr_t)workspace % 16 != 0)
+  if (need && (!workspace || workspace_bytes < need || (uintptr_t)workspace % 16 != 0))
     return fail(XATTN_ERR_WORKSPACE, "a 16-byte aligned workspace of %zu bytes needed, %zu given",
                 need, workspace ? workspace_bytes : (size_t)0);
   return launched(launch_evict(c, cache->type == XATTN_CACHE_E4M3, batch, lens, weights, budget,

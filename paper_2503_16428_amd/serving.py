@@ -343,9 +343,11 @@ def xattn_cache_evict(cache: KVCache, table, lens, weights, new_table, budget: i
             new_weights = weights.new_empty((b, h, new_width * cache.page))
         if workspace is None:
             need = _evict_bytes(h, cache.page, b, width)
-            workspace = lens.new_empty((need,), dtype=torch.uint8)
+            if need:
+                workspace = lens.new_empty((need,), dtype=torch.uint8)
     _check(lib().xattn_cache_evict(cache._ref, b, _ptr(table), width, _ptr(lens), _ptr(weights),
                                    budget, int(recent), _ptr(new_table), new_width, _ptr(kept),
                                    _ptr(new_lens), _ptr(new_weights), _ptr(workspace),
-                                   workspace.numel(), _handle(stream, at)))
+                                   0 if workspace is None else workspace.numel(),
+                                   _handle(stream, at)))
     return kept, new_lens, new_weights

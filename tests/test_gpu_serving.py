@@ -492,7 +492,7 @@ def test_scales_far_apart():
 
 def test_workspaces_may_hold_anything():
     lens = [900, 0, 77, 2000]
-    q, k, v, s, table = decode_case(4, 20, 1, 32, lens, False)
+    q, k, v, s, table = decode_case(4, 20, 1, 32, lens, False, columns=520)
     cache, qd, td, ld = on_gpu(k, v, s), q.cuda(), table.cuda(), ints(lens)
     w0 = torch.rand((4, 1, table.shape[1] * 32), generator=gen(230)).cuda()
     new_table = torch.zeros((4, 8), dtype=torch.int32, device="cuda") - 1  # nothing is moved
@@ -622,8 +622,11 @@ def test_evict_of_long_rows(kind):
         w = (w * 8).floor()
     elif kind == "one digit":  # weights whose upper 11 bits are the same
         w = 1.0 + w * 2.0 ** -4
-    check_evict(w, lens, 64, 1, 5000, 37, kind == "alike")
+    for columns in (313, 257, 256, 129, 128):  # by three launches from 257 on, else by one
+        x, n = w[..., :64 * columns].contiguous(), [min(n, 64 * columns) for n in lens]
+        check_evict(x, n, 64, 1, 5000, 37, kind == "alike")
     check_evict(w, lens, 64, 1, 90, 0, False)
+    check_evict(w[:1, :, :16000].contiguous(), [15990], 64, 1, 15989, 0, False)
 
 
 def test_evict_with_missing_pages():

@@ -172,12 +172,13 @@ def test_evict_refuses(kw):
 
 
 def test_evict_refuses_workspaces():
-    n = ctypes.c_size_t(0)
-    assert X.lib().xattn_evict_workspace_size(c_cache(), 1, 2, ctypes.byref(n)) == 0
+    n, size = ctypes.c_size_t(0), X.lib().xattn_evict_workspace_size
+    assert size(c_cache(), 1, 1024, ctypes.byref(n)) == 0 and n.value == 0  # 16384 tokens
+    assert size(c_cache(), 1, 1025, ctypes.byref(n)) == 0 and n.value > 16400 * 2 * 4
     for kw in (dict(ws=None), dict(bytes=n.value - 1), dict(ws=FAKE + 8)):
-        refused(evict(**kw), B.XATTN_ERR_WORKSPACE)
-    refused(X.lib().xattn_evict_workspace_size(c_cache(), 1, 2, None))
-    refused(X.lib().xattn_evict_workspace_size(c_cache(), 0, 2, ctypes.byref(n)))
+        refused(evict(pages=1025, **kw), B.XATTN_ERR_WORKSPACE)
+    refused(size(c_cache(), 1, 2, None))
+    refused(size(c_cache(), 0, 2, ctypes.byref(n)))
     expect("workspace must be", X.xattn_cache_evict, HostCache(), i32(3, 2), i32(3),
            torch.zeros(3, 2, 32), i32(3, 1), 4, 1, workspace=torch.zeros(8))
 
