@@ -413,7 +413,8 @@ int xattn_cache_append(const void *k, const int64_t *k_strides, const void *v,
  *   q        bf16 [batch][hq][128]; o the same (output)
  *   lens     int32 [batch] device
  *   lse      fp32 [batch][hq] (output) or NULL
- *   weights  fp32 [batch][hkv][table_pages * page] (updated) or NULL: entry t of
+ *   weights  fp32 [batch][hkv][table_pages * page], 16-byte aligned (updated), or
+ *            NULL: entry t of
  *            a key head grows by the sum of its query heads' softmax_t, for
  *            t < lens[b]; what lies behind is left as it was
  *   workspace  at least xattn_decode_workspace_size() bytes (`weights`: whether

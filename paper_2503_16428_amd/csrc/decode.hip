@@ -588,10 +588,20 @@ __device__ __forceinline__ void add_weights(const DecodeParams& p, int chunk, in
   const int b = seq_head / p.c.hkv, h = seq_head % p.c.hkv, capacity = p.c.capacity();
   const int len = len_of(p, b), t = chunk * kWeightKeys + 4 * (int)threadIdx.x;
   if (chunk * kWeightKeys >= len) return;
+  // rows are multiples of 16 keys, so that four can be read at the end too
+  float* to = weights + (long long)seq_head * capacity + t;
   f32x4 w = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (t < len) w = *(const f32x4*)to;
   for (int tile = 0; tile < p.row_tiles; ++tile) {
     const int heads = min(p.tile_rows, p.group - tile * p.tile_rows);
     const long long first = (long long)b * p.hq + h * p.group + tile * p.tile_rows;
+    // the first heads' products are on the way while the sums are found
+    constexpr int kAhead = 8;
+    const float* z = p.z + first * capacity + t;
+    f32x4 u[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (i < heads && t < len) u[i] = *(const f32x4*)(z + (size_t)i * capacity);
     const Parts parts = parts_of(p, b, h * p.row_tiles + tile);
     float top = kMinusInf, sum = 0.f;
     if (r < heads) {
@@ -621,19 +631,26 @@ __device__ __forceinline__ void add_weights(const DecodeParams& p, int chunk, in
     }
     __syncthreads();
     if (t >= len) continue;
-    const float* z = p.z + first * capacity + t;
-#pragma unroll 8
-    for (int i = 0; i < heads; ++i) {
-      const f32x4 u = *(const f32x4*)(z + (size_t)i * capacity);
+    f32x4 sums = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto add = [&](f32x4 x, int i) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] += fast_exp2(u[e] - stat[i][0]) * stat[i][1];
-    }
+      for (int e = 0; e < 4; ++e) sums[e] += fast_exp2(x[e] - stat[i][0]) * stat[i][1];
+    };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (i < heads) add(u[i], i);
+#pragma unroll 4
+    for (int i = kAhead; i < heads; ++i) add(*(const f32x4*)(z + (size_t)i * capacity), i);
+    w += sums;
   }
   if (t >= len) return;
-  float* to = weights + (long long)seq_head * capacity + t;
+  if (t + 4 <= len) {
+    *(f32x4*)to = w;
+    return;
+  }
 #pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (t + e < len) to[e] += w[e];
+  for (int e = 0; e < 3; ++e)
+    if (t + e < len) to[e] = w[e];
 }
 
 // The first batch * hq workgroups join a head each; the others add the weights.

@@ -225,7 +225,8 @@ int xattn_decode(const void* q, const xattn_cache* cache, int batch, int hq,
   CacheParams c;
   if ((rc = check_decode(cache, batch, hq, table, table_pages, &c)) ||
       (rc = check_pointer(q, "q", 16)) || (rc = check_pointer(o, "o", 16)) ||
-      (rc = check_pointer(lens, "lens", 4)) || (rc = check_cache_arrays(cache, table)))
+      (rc = check_pointer(lens, "lens", 4)) || (rc = check_cache_arrays(cache, table)) ||
+      (weights && (rc = check_pointer(weights, "weights", 16))))
     return rc;
   const size_t need = decode_scratch_bytes(c, batch, hq, weights != nullptr);
   if (!workspace || workspace_bytes < need || (uintptr_t)workspace % 16 != 0)

@@ -104,15 +104,16 @@ def test_append_refuses(kw):
 
 def decode(**kw):
     d = dict(q=FAKE, cache=c_cache(), batch=1, hq=4, table=FAKE, pages=2, lens=FAKE, o=FAKE,
-             ws=FAKE, bytes=1 << 40)
+             weights=None, ws=FAKE, bytes=1 << 40)
     d.update(kw)
     return X.lib().xattn_decode(d["q"], d["cache"], d["batch"], d["hq"], d["table"], d["pages"],
-                                d["lens"], d["o"], None, None, d["ws"], d["bytes"], None)
+                                d["lens"], d["o"], None, d["weights"], d["ws"], d["bytes"], None)
 
 
 @pytest.mark.parametrize("kw", [
     dict(q=None), dict(q=FAKE + 8), dict(o=None), dict(lens=None), dict(table=None), dict(batch=0),
     dict(hq=0), dict(hq=3), dict(pages=0), dict(pages=-1), dict(cache=None),
+    dict(weights=FAKE + 4),
     *[dict(cache=c_cache(**c)) for c in BAD_CACHES]])
 def test_decode_refuses(kw):
     refused(decode(**kw))
