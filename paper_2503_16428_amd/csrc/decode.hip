@@ -159,12 +159,14 @@ __device__ __forceinline__ int sum_of_wave(int x) {
   return x;
 }
 
-// One element of a finished row: output head `head`, element d.
+// Four elements of a finished row: output head `head`, elements d .. d + 3.
 __device__ __forceinline__ void write_row(const DecodeParams& p, long long head, int d, float top,
-                                          float sum, float out) {
+                                          float sum, f32x4 out) {
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  const __bf16 r = (__bf16)(out * inv);
-  p.o[head * kHeadDim + d] = __builtin_bit_cast(uint16_t, r);
+  typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4;
+  const bf16x4 r = {(__bf16)(out[0] * inv), (__bf16)(out[1] * inv), (__bf16)(out[2] * inv),
+                    (__bf16)(out[3] * inv)};
+  *(bf16x4*)(p.o + head * kHeadDim + d) = r;
   if (d != 0) return;
   if (p.lse) p.lse[head] = sum == 0.f ? kMinusInf : (top + log2f(sum)) / kLog2e;
   if (p.stat) {
@@ -178,7 +180,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(Decod
   constexpr int TILES = kTiles, KP = E4M3 ? 2 : 4;  // 16-byte pieces of a lane's key
   constexpr int STEP = TILES * kTile;
   using Piece = typename PieceOf<E4M3>::type;  // 8 values
-  __shared__ float so[kWaves][RT * kRows][kHeadDim + 4];
+  __shared__ __attribute__((aligned(16))) float so[kWaves][RT * kRows][kHeadDim + 4];
   __shared__ float sm[kWaves][RT * kRows], sl[kWaves][RT * kRows];
   const int tid = threadIdx.x, lane = tid % kWave;
   const unsigned g = lane / 16, c = lane % 16;
@@ -461,22 +463,24 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(Decod
     const bool done = u0 == 0 && n == row_units;  // the whole row
     const long long slot = 2ll * blockIdx.x + (first_segment ? 0 : 1);
     const int rows = min(RT * kRows, heads);
-    for (int i = fresh(tid); i < rows * kHeadDim; i += kThreads) {
-      const int rq = i / kHeadDim, d = i % kHeadDim;
+    constexpr int kLanes = kHeadDim / 4;  // threads of a head, four elements each
+    for (int i = fresh(tid); i < rows * kLanes; i += kThreads) {
+      const int rq = i / kLanes, d = i % kLanes * 4;
       float top = sm[0][rq];
 #pragma unroll
       for (int w = 1; w < kWaves; ++w) top = fmaxf(top, sm[w][rq]);
-      float sum = 0.f, out = 0.f;
+      float sum = 0.f;
+      f32x4 out = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
         const float f = weight_of(sm[w][rq], top);
         sum += f * sl[w][rq];
-        out += f * so[w][rq][d];
+        out += f * *(const f32x4*)&so[w][rq][d];
       }
       if (done) {
         write_row(p, (long long)b * p.hq + h * p.group + tile * RT * kRows + rq, d, top, sum, out);
       } else {
-        p.part[(slot * p.tile_rows + rq) * kHeadDim + d] = out;
+        *(f32x4*)(p.part + (slot * p.tile_rows + rq) * kHeadDim + d) = out;
         if (d == 0) {
           p.ml[(slot * p.tile_rows + rq) * 2] = top;
           p.ml[(slot * p.tile_rows + rq) * 2 + 1] = sum;
@@ -519,17 +523,17 @@ __device__ __forceinline__ Parts parts_of(const DecodeParams& p, int b, int row)
 
 // Threads of decode_join: half as many are 2 us faster for 2048 heads, others alike.
 constexpr int kJoin = 128, kJoinWaves = kJoin / kWave;
-// One workgroup per query head: the parts of its row, if it has any, eight at a
-// time, 32 lanes of 4 elements each, then the eight sums in order.
+// One workgroup per query head: the parts of its row, if it has any, four at a
+// time, 32 lanes of 4 elements each, then the four sums in order.
 __device__ __forceinline__ void join(const DecodeParams& p, int head) {
   constexpr int kLanes = kHeadDim / 4, kAtOnce = kJoin / kLanes;
-  __shared__ float so[kAtOnce][kHeadDim];
+  __shared__ __attribute__((aligned(16))) float so[kAtOnce][kHeadDim];
   __shared__ float sf[kMostWorkers], sl[kMostWorkers], st[kJoinWaves];
   const int tid = threadIdx.x, b = head / p.hq, hq = head % p.hq;
   const int h = hq / p.group, in_group = hq % p.group;
   const int tile = in_group / p.tile_rows, r = in_group % p.tile_rows;
   if (len_of(p, b) == 0) {
-    if (tid < kHeadDim) write_row(p, head, tid, 0.f, 0.f, 0.f);
+    if (tid < kLanes) write_row(p, head, 4 * tid, 0.f, 0.f, f32x4{0.f, 0.f, 0.f, 0.f});
     return;
   }
   const Parts parts = parts_of(p, b, h * p.row_tiles + tile);
@@ -567,20 +571,20 @@ __device__ __forceinline__ void join(const DecodeParams& p, int head) {
   }
   *(f32x4*)&so[part][d] = out;
   __syncthreads();
-  if (tid >= kHeadDim) return;
-  float o = 0.f;
+  if (tid >= kLanes) return;
+  out = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int i = 0; i < kAtOnce; ++i) o += so[i][tid];
+  for (int i = 0; i < kAtOnce; ++i) out += *(const f32x4*)&so[i][d];
   sum = 0.f;
 #pragma unroll
   for (int i = 0; i < kJoinWaves; ++i) sum += st[i];
-  write_row(p, head, tid, top, sum, o);
+  write_row(p, head, d, top, sum, out);
 }
 
 constexpr int kWeightKeys = 4 * kJoin;  // keys of a workgroup's weights
 
-// The weights of 1024 keys of a key head, from the products, a tile of its heads
-// after the other. First the heads' maxima and sums, eight lanes a head.
+// The weights of 512 keys of a key head, from the products, a tile of its heads
+// after the other. First the heads' maxima and sums, four lanes a head.
 __device__ __forceinline__ void add_weights(const DecodeParams& p, int chunk, int seq_head,
                                             float* __restrict__ weights) {
   __shared__ float stat[2 * kRows][2];

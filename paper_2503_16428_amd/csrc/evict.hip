@@ -107,7 +107,7 @@ __device__ __forceinline__ void find(SelectShared& s, const int* hist, int parts
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int low = kBins - 2 - 2 * tid;  // this thread's bins: low + 1, low
   int n0 = 0, n1 = 0;
-#pragma unroll 8
+#pragma unroll 16
   for (int i = 0; i < parts; ++i) {
     const int2 x = *(const int2*)(hist + (size_t)i * stride + low);
     n0 += x.y;
