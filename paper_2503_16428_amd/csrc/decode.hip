@@ -188,14 +188,16 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(Decod
   const uint32_t k_off = c * (E4M3 ? 128 : 256) + 16 * g;
   const uint32_t v_off = E4M3 ? 512 * g + 8 * c : 1024 * g + 16 * c;
   const int wave = uniform(tid / kWave);
-  const int per_seq = p.c.hkv * p.row_tiles;
-
   // This workgroup's share, and the sequence that it begins in. Every wave finds
   // out for itself, without a barrier: its lanes have equal runs of the batch.
   const int run = (p.batch + kWave - 1) / kWave;
   const int b0 = min(lane * run, p.batch), b1 = min(b0 + run, p.batch);
-  int mine = 0;
-  for (int i = b0; i < b1; ++i) mine += units_of(p, i);
+  const int per_row = p.c.hkv * p.row_tiles;
+  int mine = 0, len = 0;
+  for (int i = b0; i < b1; ++i) {
+    len = len_of(p, i);
+    mine += (len + kUnit - 1) / kUnit * per_row;
+  }
   int before = mine;
 #pragma unroll
   for (int off = 1; off < kWave; off <<= 1) {
@@ -209,18 +211,23 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(Decod
   const int holder = __ffsll((unsigned long long)__ballot(begin < before)) - 1;
   int b = b0;
   int at = begin - (before - mine);  // units into sequence b
-  if (lane == holder)
-    for (int u; at >= (u = units_of(p, b)); ++b) at -= u;
+  if (lane == holder && run > 1)
+    for (;; ++b) {
+      len = len_of(p, b);
+      const int u = (len + kUnit - 1) / kUnit * per_row;
+      if (at < u) break;
+      at -= u;
+    }
   b = __builtin_amdgcn_readlane(b, holder);
   at = __builtin_amdgcn_readlane(at, holder);
+  len = __builtin_amdgcn_readlane(len, holder);
   bool first_segment = true;
 
   while (left > 0) {
-    const int len = uniform(len_of(p, b));
     const int row_units = (len + kUnit - 1) / kUnit;
-    if (at >= row_units * per_seq) {
+    if (at >= row_units * per_row) {
       at = 0;
-      ++b;
+      len = uniform(len_of(p, ++b));
       continue;
     }
     const int row = at / row_units, u0 = at - row * row_units, n = min(left, row_units - u0);
