@@ -10,6 +10,11 @@
 // computes
 // its token's eight angles once, while its first vector is on the way, and loads
 // the next head's before it turns this one.
+//
+// Bound by HBM, every vector read and written once: 32K tokens of 32 heads 102 us
+// (537 MB, 5.3 TB/s; a copy of that size 5.1), 115,200 of 24 heads 251 us (1.42 GB,
+// 5.7 TB/s), append of 48,542 tokens of 8 heads in e4m3 55 us (5.4 TB/s); one token
+// of 64 sequences 4 us, a chain of loads.
 #include <type_traits>
 
 #include "serve.h"
