@@ -10,9 +10,9 @@
 //     those same keys, so that the i-th elements of its 8 pieces are row c of the
 //     A operand of MFMA i, whose output rows are elements 8c + i: pairs of values
 //     are put together within the lane, nothing moves between lanes.
-// P is the sum of two bf16 values (16 bits of mantissa, products exact), one MFMA
-// each: the product is as good as fp32 for an output in bf16, at an eighth of
-// the time of fp32 MFMAs.
+// P is the sum of two bf16 values, one MFMA each (products exact): the weights are
+// off by at most 2^-15, less than a hundredth of the output's own rounding, at an
+// eighth of the time of fp32 MFMAs.
 //
 // The work of a batch is its rows (sequence, key head, tile of query heads) end
 // to end, in units of kWaves wave steps; every workgroup takes an equal share of
@@ -57,12 +57,13 @@ __device__ __forceinline__ bf16x8 bf16_of(uint32_t a, uint32_t b) {
   const auto s = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true);
   return bf16x8{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
 }
-// The two bf16 values of p and q whose sums they are: the upper halves of their
-// bits, and what is left, rounded. The rest is made 2^-17 p too large, so that it
-// is positive and an infinite value times p is infinite.
+// The two bf16 values of p and q whose sums stand for p (1 + 2^-17): the upper
+// halves of their bits, and what is left, at most 2^-7 p, rounded by at most 2^-8 of
+// it. The rest is made 2^-17 p larger so that it is positive, and an infinite value
+// times p infinite; the factor goes out with the sum of the weights.
+constexpr float kMore = 1.f + 0x1p-17f;
 __device__ __forceinline__ void split(float p, float q, uint32_t* upper, uint32_t* rest) {
   const uint32_t a = __builtin_bit_cast(uint32_t, p), b = __builtin_bit_cast(uint32_t, q);
-  constexpr float kMore = 1.f + 0x1p-17f;
   typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
   const bf16x2 r = {
       (__bf16)__builtin_fmaf(p, kMore, -__builtin_bit_cast(float, a & 0xffff0000u)),
@@ -166,10 +167,11 @@ __device__ __forceinline__ int sum_of_wave(int x) {
   return x;
 }
 
-// Four elements of a finished row: output head `head`, elements d .. d + 3.
+// Four elements of a finished row: output head `head`, elements d .. d + 3, from the
+// sum of its values times kMore.
 __device__ __forceinline__ void write_row(const DecodeParams& p, long long head, int d, float top,
                                           float sum, f32x4 out) {
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const float inv = sum == 0.f ? 0.f : 1.f / (kMore * sum);
   typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4;
   const bf16x4 r = {(__bf16)(out[0] * inv), (__bf16)(out[1] * inv), (__bf16)(out[2] * inv),
                     (__bf16)(out[3] * inv)};

@@ -106,7 +106,9 @@ def decode(q, k, v, table, lens, k_scale=None, v_scale=None):
             dz += float(z[use].abs().max()) * 4 * 2.0 ** -24
             # the exponential's 2^-22 and at most n + 8 roundings of the sums and joins
             rel = 2 * dz + 2.0 ** -20 + (n + 8) * 2.0 ** -24
-            ob[b, h] = (p[use] @ vv[g][use].abs()) * 2 * rel
+            # P in the product is two bf16 parts: the upper 8 bits of mantissa leave at
+            # most 2^-7 of it, whose rounding to 8 bits is off by at most 2^-8 of that
+            ob[b, h] = (p[use] @ vv[g][use].abs()) * (2 * rel + 2.0 ** -15)
             lb[b, h] = dz + 2.0 ** -20 + (n + 8) * 2.0 ** -24 + abs(float(lse[b, h])) * 2.0 ** -22
             wb[b, g, :n] += p * 2 * rel
     return o, lse, w, ob, lb, wb

@@ -2,6 +2,7 @@
 (tests/serving_oracle.py): rotary positions, the append to the paged cache, one
 new token's attention, eviction; and a run of them together behind a prefill."""
 import math
+import random
 
 import pytest
 
@@ -344,6 +345,27 @@ def test_decode_of_many_short_sequences():
     check_decode(*decode_case(150, 4, 1, 16, lens, False), lens)
 
 
+def test_decode_of_more_sequences_than_lanes():
+    lens = [(7 * i) % 5 if i % 97 else 200 for i in range(1000)]
+    check_decode(*decode_case(1000, 1, 1, 16, lens, False, spare=0, columns=13), lens)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_decode_of_random_shapes(seed):
+    rng = random.Random(seed)
+    hkv = rng.choice([1, 1, 2, 3, 5, 8])
+    hq = hkv * rng.choice([1, 2, 4, 5, 7, 8, 15, 16, 18, 32, 33, 65])
+    page, batch = rng.choice([16, 32, 64, 128, 256]), rng.choice([1, 2, 3, 7, 20, 70])
+    most = int(math.exp(rng.uniform(0, math.log(40000 / batch / max(1, hq // 16)))))
+    lens = [rng.choice([0, 1, most, rng.randint(0, most)]) for _ in range(batch)]
+    lens[rng.randrange(batch)] = most
+    print(f"{batch=} {hq=} {hkv=} {page=} {most=}", flush=True)
+    q, k, v, s, table = decode_case(batch, hq, hkv, page, lens, rng.random() < 0.5, seed=300 + seed)
+    if rng.random() < 0.3:
+        table[torch.rand(table.shape, generator=gen(400 + seed)) < 0.1] = -1
+    check_decode(q, k, v, s, table, lens)
+
+
 def test_decode_of_lengths_past_the_table():
     """Lengths outside 0 .. capacity count as its ends."""
     q, k, v, s, table = decode_case(3, 4, 2, 16, [48], False, columns=3)
@@ -627,6 +649,21 @@ def test_evict_of_long_rows(kind):
         check_evict(x, n, 64, 1, 5000, 37, kind == "alike")
     check_evict(w, lens, 64, 1, 90, 0, False)
     check_evict(w[:1, :, :16000].contiguous(), [15990], 64, 1, 15989, 0, False)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_evict_of_random_shapes(seed):
+    rng = random.Random(500 + seed)
+    page, batch, hkv = rng.choice([16, 64, 256]), rng.choice([1, 2, 5]), rng.choice([1, 2, 3])
+    most = int(math.exp(rng.uniform(math.log(2), math.log(24000 / batch / hkv))))
+    lens = [most] + [rng.randint(0, most) for _ in range(batch - 1)]
+    budget = rng.randint(1, min(most, 3000))
+    print(f"{batch=} {hkv=} {page=} {lens=} {budget=}", flush=True)
+    columns = -(-most // page) + rng.randint(0, 2)
+    w = torch.randn((batch, hkv, columns * page), generator=gen(600 + seed))
+    if rng.random() < 0.5:
+        w = w.clamp(min=0)  # half of them alike
+    check_evict(w, lens, page, hkv, budget, rng.randint(0, budget), rng.random() < 0.5)
 
 
 def test_evict_with_missing_pages():
