@@ -143,13 +143,15 @@ struct Shares {
   int workers, per, more;
   __device__ Shares(int units, int most) {
     workers = min((units + 1) / 2, most);
-    per = workers ? units / workers : 0;
+    per = workers ? (unsigned)units / (unsigned)workers : 0;
     more = units - workers * per;
   }
   __device__ int first(int worker) const { return worker * per + min(worker, more); }
   __device__ int worker_of(int unit) const {
     const int early = more * (per + 1);
-    return unit < early ? unit / (per + 1) : more + (unit - early) / per;
+    const bool is_early = unit < early;
+    const unsigned from = is_early ? unit : unit - early;
+    return (int)(from / (unsigned)(is_early ? per + 1 : per)) + (is_early ? 0 : more);
   }
 };
 
@@ -161,10 +163,19 @@ __device__ __forceinline__ int units_of(const DecodeParams& p, int b) {
   return (len_of(p, b) + kUnit - 1) / kUnit * (p.c.hkv * p.row_tiles);
 }
 
-__device__ __forceinline__ int sum_of_wave(int x) {
-#pragma unroll
-  for (int off = 1; off < kWave; off <<= 1) x += __shfl_xor(x, off);
+// Sums over the wave's lanes up to this one, by moves within rows of 16 lanes and
+// from row to row: short code, which every launch fetches anew.
+__device__ __forceinline__ int scan_of_wave(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // 1, 2, 4, 8 lanes up
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // lane 15 of rows 0, 2 up
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to rows 2, 3
   return x;
+}
+__device__ __forceinline__ int sum_of_wave(int x) {
+  return __builtin_amdgcn_readlane(scan_of_wave(x), kWave - 1);
 }
 
 // Four elements of a finished row: output head `head`, elements d .. d + 3, from the
@@ -207,12 +218,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(Decod
     len = len_of(p, i);
     mine += (len + kUnit - 1) / kUnit * per_row;
   }
-  int before = mine;
-#pragma unroll
-  for (int off = 1; off < kWave; off <<= 1) {
-    const int up = __shfl_up(before, off);
-    if (lane >= off) before += up;
-  }
+  const int before = scan_of_wave(mine);
   const Shares shares(__builtin_amdgcn_readlane(before, kWave - 1), p.most_workers);
   if ((int)blockIdx.x >= shares.workers) return;
   const int begin = shares.first(blockIdx.x);
@@ -239,8 +245,11 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(Decod
       len = uniform(len_of(p, ++b));
       continue;
     }
-    const int row = at / row_units, u0 = at - row * row_units, n = min(left, row_units - u0);
-    const int h = row / p.row_tiles, tile = row % p.row_tiles;
+    const int row = (unsigned)at / (unsigned)row_units, u0 = at - row * row_units;
+    const int n = min(left, row_units - u0);
+    // groups of one tile of MFMA columns are one tile
+    const int h = RT == 1 ? row : (unsigned)row / (unsigned)p.row_tiles;
+    const int tile = RT == 1 ? 0 : row - h * p.row_tiles;
     const int t0 = u0 * kUnit, t1 = min((u0 + n) * kUnit, len);
 
     bf16x8 q[RT][4];
@@ -527,9 +536,9 @@ __device__ __forceinline__ Parts parts_of(const DecodeParams& p, int b, int row)
     all += u;
     if (i < b) before += u;
   }
-  const Shares shares(uniform(sum_of_wave(all)), p.most_workers);
+  const Shares shares(sum_of_wave(all), p.most_workers);
   const int row_units = (len_of(p, b) + kUnit - 1) / kUnit;
-  const int start = uniform(sum_of_wave(before)) + row * row_units;
+  const int start = sum_of_wave(before) + row * row_units;
   Parts r;
   r.first = shares.worker_of(start);
   r.last = shares.worker_of(start + row_units - 1);
