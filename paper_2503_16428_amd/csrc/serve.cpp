@@ -55,7 +55,7 @@ int check_strides(const int64_t* s, const char* name, int batch, int heads, int 
   return XATTN_OK;
 }
 
-constexpr double kTwoPi = 6.283185307179586476925286766559;
+constexpr double kTurn = 0.15915494309189533576888;  // 1 / 2 pi
 
 int check_plan(const xattn_rotary_plan* plan, RotaryParams* out) {
   if (!plan) return fail(XATTN_ERR_ARG, "plan is NULL");
@@ -71,12 +71,16 @@ int check_plan(const xattn_rotary_plan* plan, RotaryParams* out) {
     if (a < plan->axes ? pairs < 1 || pairs > 64 : pairs != 0)
       return fail(XATTN_ERR_ARG, "pairs[%d] = %d with %d axes", a, pairs, plan->axes);
     if (n + pairs > 64) return fail(XATTN_ERR_ARG, "more than 64 pairs");
-    for (int i = 0; i < pairs; ++i, ++n) {
-      if (!std::isfinite(plan->freq[n])) return fail(XATTN_ERR_ARG, "freq[%d] is not finite", n);
-      out->turn[n] = plan->freq[n] / kTwoPi;
-    }
+    n += pairs;
     if (a < 2) out->end[a] = n;
   }
+  // 0 * x is 0 unless x is infinite or NaN
+  double finite = 0.0;
+  for (int i = 0; i < n; ++i) {
+    out->turn[i] = plan->freq[i] * kTurn;
+    finite += 0.0 * plan->freq[i];
+  }
+  if (!(finite == 0.0)) return fail(XATTN_ERR_ARG, "a frequency is not finite");
   out->axes = plan->axes;
   out->n = n;
   return XATTN_OK;

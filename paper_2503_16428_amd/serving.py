@@ -13,7 +13,6 @@ Tensor layouts:
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import functools
 
@@ -58,7 +57,6 @@ class Rotary:
                                 self._freq.ctypes.data)
         self.axes = len(pairs)
         self._ref = ctypes.byref(self._plan)
-
 
 
 class KVCache:
@@ -129,9 +127,14 @@ def _is(t, shape, dtype, name):
         _check_shape(t, shape, dtype, name)
 
 
+@functools.lru_cache(maxsize=1024)
+def _strides(batch, head, token):
+    return _I3(batch, head, token)  # only ever read
+
+
 def _vectors(t, name, like=None):
     """(batch, heads, tokens, strides) of bf16 vectors, checked but for the device."""
-    if t.dtype != torch.bfloat16:
+    if t.dtype is not torch.bfloat16:
         _fail(f"{name} must be torch.bfloat16, got {t.dtype}")
     shape, strides = t.shape, t.stride()
     if len(shape) == 3:
@@ -143,7 +146,7 @@ def _vectors(t, name, like=None):
         _fail(f"{name} must have shape {tuple(like.shape)}, got {tuple(t.shape)}")
     if strides[3] != 1:
         _fail(f"the {HEAD_DIM} values of a vector of {name} must be contiguous")
-    return shape[0], shape[1], shape[2], _I3(*strides[:3])
+    return shape[0], shape[1], shape[2], _strides(*strides[:3])
 
 
 def _positions(pos, rotary, batch, tokens, dims):
@@ -159,10 +162,13 @@ def _is_cache(cache):
 
 
 def _table(table, batch, name="table"):
-    if table.dim() != 2 or table.shape[0] != batch or table.shape[1] < 1:
-        _fail(f"{name} must be [{batch}, pages], got {tuple(table.shape)}")
-    if table.dtype != torch.int32:
+    """Columns of a page table of `batch` rows."""
+    shape = table.shape
+    if len(shape) != 2 or shape[0] != batch or shape[1] < 1:
+        _fail(f"{name} must be [{batch}, pages], got {tuple(shape)}")
+    if table.dtype is not torch.int32:
         _fail(f"{name} must be torch.int32, got {table.dtype}")
+    return shape[1]
 
 
 def _extent(t):
@@ -176,9 +182,12 @@ def _apart(a, b):
     return a1 <= b0 or b1 <= a0
 
 
-def _allocating(stream):
-    """What a call allocates belongs to the stream that it runs on."""
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+def _made(stream, allocate):
+    """What `allocate` makes, of the memory of the stream that the call runs on."""
+    if stream is None:
+        return allocate()
+    with torch.cuda.stream(stream):
+        return allocate()
 
 
 def _handle(stream, at):
@@ -196,12 +205,9 @@ def xattn_rotary(x, pos, rotary: Rotary, inverse=False, out=None, stream=None):
     _positions(pos, rotary, b, n, x.dim())
     if out is None:
         at = _here(x, (pos,), ("x", "pos"), (pos,))
-        if stream is None:
-            out = x.new_empty(x.shape)
-        else:
-            with _allocating(stream):
-                out = x.new_empty(x.shape)
-        os = _I3(h * n * HEAD_DIM, n * HEAD_DIM, HEAD_DIM)
+        out = x.new_empty(x.shape) if stream is None else _made(
+            stream, lambda: x.new_empty(x.shape))
+        os = _strides(h * n * HEAD_DIM, n * HEAD_DIM, HEAD_DIM)
     else:
         _, _, _, os = _vectors(out, "out", x)
         at = _here(x, (out, pos), ("x", "out", "pos"), (pos,))
@@ -222,7 +228,7 @@ def xattn_cache_append(k, v, cache: KVCache, table, start, count=None, pos=None,
     _, _, _, vs = _vectors(v, "v", k)
     if h != cache.hkv:
         _fail(f"k has {h} heads, the cache {cache.hkv}")
-    _table(table, b)
+    width = _table(table, b)
     _is(start, (b,), torch.int32, "start")
     _is(count, (b,), torch.int32, "count")
     if (pos is None) != (rotary is None):
@@ -231,8 +237,8 @@ def xattn_cache_append(k, v, cache: KVCache, table, start, count=None, pos=None,
         _positions(pos, rotary, b, n, k.dim())
     at = _here(k, (v, table, start, count, pos, cache.k),
                ("k", "v", "table", "start", "count", "pos", "cache"), (table, start, count, pos))
-    _check(lib().xattn_cache_append(_ptr(k), ks, _ptr(v), vs, b, n, _ptr(count), _ptr(start),
-                                    _ptr(table), table.shape[1], _ptr(pos),
+    _check(lib().xattn_cache_append(k.data_ptr(), ks, v.data_ptr(), vs, b, n, _ptr(count),
+                                    start.data_ptr(), table.data_ptr(), width, _ptr(pos),
                                     None if rotary is None else rotary._ref, cache._ref,
                                     _handle(stream, at)))
 
@@ -261,31 +267,32 @@ def xattn_decode(q, cache: KVCache, table, lens, o=None, lse=None, weights=None,
     tokens: (o like q, lse fp32 [batch, hq] or None). weights (fp32 [batch, hkv,
     table_pages * page]), if given, grow by each key's softmax weights, summed over its heads."""
     _is_cache(cache)
-    if q.dim() != 3 or q.shape[2] != HEAD_DIM or 0 in q.shape:
-        _fail(f"q must be [batch, hq, {HEAD_DIM}], got {tuple(q.shape)}")
-    if q.dtype != torch.bfloat16:
+    shape = q.shape
+    if len(shape) != 3 or shape[2] != HEAD_DIM or 0 in shape:
+        _fail(f"q must be [batch, hq, {HEAD_DIM}], got {tuple(shape)}")
+    if q.dtype is not torch.bfloat16:
         _fail(f"q must be torch.bfloat16, got {q.dtype}")
-    b, hq, _ = q.shape
-    _table(table, b)
+    b, hq, _ = shape
+    width = _table(table, b)
     _is(lens, (b,), torch.int32, "lens")
-    _is(o, q.shape, torch.bfloat16, "o")
+    _is(o, shape, torch.bfloat16, "o")
     _is(lse, (b, hq), torch.float32, "lse")
-    width = table.shape[1]
     _is(weights, (b, cache.hkv, width * cache.page), torch.float32, "weights")
     _check_workspace(workspace)
     dense = (q, table, lens, o, lse, weights, workspace)
     at = _here(q, (table, lens, cache.k, o, lse, weights, workspace),
                ("q", "table", "lens", "cache", "o", "lse", "weights", "workspace"), dense)
-    with _allocating(stream):
-        if o is None:
-            o = q.new_empty(q.shape)
-        if lse is None and want_lse:
-            lse = q.new_empty((b, hq), dtype=torch.float32)
-        if workspace is None:
-            need = _decode_bytes(cache.hkv, cache.page, b, hq, width, int(weights is not None))
-            workspace = q.new_empty((need,), dtype=torch.uint8)
-    _check(lib().xattn_decode(_ptr(q), cache._ref, b, hq, _ptr(table), width, _ptr(lens), _ptr(o),
-                              _ptr(lse), _ptr(weights), _ptr(workspace), workspace.numel(),
+    def allocate():
+        need = 0 if workspace is not None else _decode_bytes(cache.hkv, cache.page, b, hq, width,
+                                                             int(weights is not None))
+        return (q.new_empty(shape) if o is None else o,
+                q.new_empty((b, hq), dtype=torch.float32) if lse is None and want_lse else lse,
+                q.new_empty((need,), dtype=torch.uint8) if workspace is None else workspace)
+
+    o, lse, workspace = _made(stream, allocate)
+    _check(lib().xattn_decode(q.data_ptr(), cache._ref, b, hq, table.data_ptr(), width,
+                              lens.data_ptr(), o.data_ptr(), _ptr(lse), _ptr(weights),
+                              workspace.data_ptr(), workspace.numel(),
                               _handle(stream, at)))
     return o, lse
 
@@ -314,12 +321,10 @@ def xattn_cache_evict(cache: KVCache, table, lens, weights, new_table, budget: i
     _is_cache(cache)
     if table.dim() != 2:
         _fail(f"table must be [batch, pages], got {tuple(table.shape)}")
-    b, h, width, budget = table.shape[0], cache.hkv, table.shape[1], int(budget)
-    _table(table, b)
-    _table(new_table, b, "new_table")
+    b, h, budget = table.shape[0], cache.hkv, int(budget)
+    width, new_width = _table(table, b), _table(new_table, b, "new_table")
     _is(lens, (b,), torch.int32, "lens")
     _is(weights, (b, h, width * cache.page), torch.float32, "weights")
-    new_width = new_table.shape[1]
     if not 1 <= budget <= new_width * cache.page:
         _fail(f"budget must be 1 to {new_width * cache.page} (the new table's tokens), got "
               f"{budget}")
@@ -334,17 +339,15 @@ def xattn_cache_evict(cache: KVCache, table, lens, weights, new_table, budget: i
     for n, out, given in (("new_lens", new_lens, lens), ("new_weights", new_weights, weights)):
         if out is not None and not _apart(out, given):
             _fail(f"{n} must lie apart from the call's input")
-    with _allocating(stream):
-        if kept is None:
-            kept = lens.new_empty((b, h, budget))
-        if new_lens is None:
-            new_lens = lens.new_empty((b,))
-        if new_weights is None:
-            new_weights = weights.new_empty((b, h, new_width * cache.page))
-        if workspace is None:
-            need = _evict_bytes(h, cache.page, b, width)
-            if need:
-                workspace = lens.new_empty((need,), dtype=torch.uint8)
+    def allocate():
+        need = 0 if workspace is not None else _evict_bytes(h, cache.page, b, width)
+        return (lens.new_empty((b, h, budget)) if kept is None else kept,
+                lens.new_empty((b,)) if new_lens is None else new_lens,
+                weights.new_empty((b, h, new_width * cache.page)) if new_weights is None
+                else new_weights,
+                lens.new_empty((need,), dtype=torch.uint8) if need else workspace)
+
+    kept, new_lens, new_weights, workspace = _made(stream, allocate)
     _check(lib().xattn_cache_evict(cache._ref, b, _ptr(table), width, _ptr(lens), _ptr(weights),
                                    budget, int(recent), _ptr(new_table), new_width, _ptr(kept),
                                    _ptr(new_lens), _ptr(new_weights), _ptr(workspace),
