@@ -25,7 +25,7 @@
 // of bf16 keys and values, which keeps the matrix cores busy for 6 % of the time
 // that the loads take. 64 sequences of up to 8000 tokens, 32 / 8 heads, 1.08 GB:
 // 170 us in decode_kernel (6.3 TB/s; a kernel that only loads does 6.2 to 7.0), 5.6
-// in decode_join; one of 128K 82 + 5; e4m3, 16 of up to 20,011, 28 / 4 heads, with
+// in decode_join; one of 128K 81 + 5; e4m3, 16 of up to 20,011, 28 / 4 heads, with
 // weights 37 + 9. About 6 us of each are the chain of first loads and the end.
 #include "serve.h"
 
