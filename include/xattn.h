@@ -418,8 +418,9 @@ int xattn_cache_append(const void *k, const int64_t *k_strides, const void *v,
  *            a key head grows by the sum of its query heads' softmax_t, for
  *            t < lens[b]; what lies behind is left as it was
  *   workspace  at least xattn_decode_workspace_size() bytes (`weights`: whether
- *            the call has them), 16-byte aligned; its contents on entry are
- *            ignored. Calls that may run at the same time need one each.
+ *            the call has them; 0 for small calls, then it may be NULL), 16-byte
+ *            aligned; its contents on entry are ignored. Calls that may run at the
+ *            same time need one each.
  * QK^T and PV run on the bf16 matrix cores with fp32 accumulation (e4m3 values
  * are exact in bf16); the softmax is fp32, and P goes into PV as the sum of two
  * bf16 values, within 2^-15 of it. The output is rounded once.

@@ -14,12 +14,12 @@
 // off by at most 2^-15, less than a hundredth of the output's own rounding, at an
 // eighth of the time of fp32 MFMAs.
 //
-// The work of a batch is its rows (sequence, key head, tile of query heads) end
-// to end, in units of kWaves wave steps; every workgroup takes an equal share of
-// the units, whatever the lengths, and goes through the rows in it. A row that
-// one workgroup has whole is done there; of the others every share leaves a
-// partial output (at most two a workgroup: its first and its last row), and
-// decode_join adds them in order.
+// Short rows (sequence, key head, tile of query heads) are one workgroup's each. The
+// work of longer ones is the batch's rows end to end, in units of kWaves wave steps;
+// every workgroup takes an equal share of the units, whatever the lengths, and goes
+// through the rows in it. A row that one workgroup has whole is done there; of the
+// others every share leaves a partial output (at most two a workgroup: its first and
+// its last row), and decode_join adds them in order.
 //
 // Bound by HBM: with tiles filled up to 16 heads and P in two parts 24 flops a byte
 // of bf16 keys and values, which keeps the matrix cores busy for 6 % of the time
@@ -110,7 +110,8 @@ struct DecodeParams {
   const int32_t* lens;
   uint16_t* o;
   float* lse;    // or NULL
-  int batch, hq, group, row_tiles, tile_rows, most_workers;
+  int batch, hq, group, row_tiles, tile_rows;
+  int most_workers;  // or 0: every row is one workgroup's
   float* part;   // [2 workers][tile_rows][128] unnormalised outputs
   float* ml;     // [2 workers][tile_rows][2] (maximum in log2, sum)
   float* stat;   // [batch][hq][2] (maximum in log2, sum) of whole rows, or NULL
@@ -195,7 +196,8 @@ __device__ __forceinline__ void write_row(const DecodeParams& p, long long head,
   }
 }
 
-template <bool E4M3, int RT>
+// WHOLE: a workgroup has a row, and nothing is left to join.
+template <bool E4M3, int RT, bool WHOLE>
 __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(DecodeParams p) {
   constexpr int TILES = kTiles, KP = E4M3 ? 2 : 4;  // 16-byte pieces of a lane's key
   constexpr int STEP = TILES * kTile;
@@ -208,34 +210,50 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(Decod
   const uint32_t k_off = c * (E4M3 ? 128 : 256) + 16 * g;
   const uint32_t v_off = E4M3 ? 512 * g + 8 * c : 1024 * g + 16 * c;
   const int wave = uniform(tid / kWave);
-  // This workgroup's share, and the sequence that it begins in. Every wave finds
-  // out for itself, without a barrier: its lanes have equal runs of the batch.
-  const int run = (p.batch + kWave - 1) / kWave;
-  const int b0 = min(lane * run, p.batch), b1 = min(b0 + run, p.batch);
   const int per_row = p.c.hkv * p.row_tiles;
-  int mine = 0, len = 0;
-  for (int i = b0; i < b1; ++i) {
-    len = len_of(p, i);
-    mine += (len + kUnit - 1) / kUnit * per_row;
-  }
-  const int before = scan_of_wave(mine);
-  const Shares shares(__builtin_amdgcn_readlane(before, kWave - 1), p.most_workers);
-  if ((int)blockIdx.x >= shares.workers) return;
-  const int begin = shares.first(blockIdx.x);
-  int left = shares.first(blockIdx.x + 1) - begin;
-  const int holder = __ffsll((unsigned long long)__ballot(begin < before)) - 1;
-  int b = b0;
-  int at = begin - (before - mine);  // units into sequence b
-  if (lane == holder && run > 1)
-    for (;; ++b) {
-      len = len_of(p, b);
-      const int u = (len + kUnit - 1) / kUnit * per_row;
-      if (at < u) break;
-      at -= u;
+  int b, at, left, len;  // the sequence, units into it, units to do, its length
+  if constexpr (WHOLE) {
+    b = (unsigned)blockIdx.x / (unsigned)per_row;
+    const int row = blockIdx.x - b * per_row;
+    len = uniform(len_of(p, b));
+    left = (len + kUnit - 1) / kUnit;
+    at = row * left;
+    if (left == 0) {  // no key
+      const int h = RT == 1 ? row : (unsigned)row / (unsigned)p.row_tiles;
+      const int first = RT == 1 ? 0 : (row - h * p.row_tiles) * RT * kRows;
+      const int rows = min(RT * kRows, p.group - first);
+      for (int i = tid; i < rows * (kHeadDim / 4); i += kThreads)
+        write_row(p, (long long)b * p.hq + h * p.group + first + i / (kHeadDim / 4),
+                  i % (kHeadDim / 4) * 4, 0.f, 0.f, f32x4{0.f, 0.f, 0.f, 0.f});
     }
-  b = __builtin_amdgcn_readlane(b, holder);
-  at = __builtin_amdgcn_readlane(at, holder);
-  len = __builtin_amdgcn_readlane(len, holder);
+  } else {
+    // This workgroup's share, and the sequence that it begins in. Every wave finds
+    // out for itself, without a barrier: its lanes have equal runs of the batch.
+    const int run = (p.batch + kWave - 1) / kWave;
+    const int b0 = min(lane * run, p.batch), b1 = min(b0 + run, p.batch);
+    int mine = 0, my_len = 0;
+    for (int i = b0; i < b1; ++i) {
+      my_len = len_of(p, i);
+      mine += (my_len + kUnit - 1) / kUnit * per_row;
+    }
+    const int before = scan_of_wave(mine);
+    const Shares shares(__builtin_amdgcn_readlane(before, kWave - 1), p.most_workers);
+    if ((int)blockIdx.x >= shares.workers) return;
+    const int begin = shares.first(blockIdx.x);
+    left = shares.first(blockIdx.x + 1) - begin;
+    const int holder = __ffsll((unsigned long long)__ballot(begin < before)) - 1;
+    int my_b = b0, my_at = begin - (before - mine);
+    if (lane == holder && run > 1)
+      for (;; ++my_b) {
+        my_len = len_of(p, my_b);
+        const int u = (my_len + kUnit - 1) / kUnit * per_row;
+        if (my_at < u) break;
+        my_at -= u;
+      }
+    b = __builtin_amdgcn_readlane(my_b, holder);
+    at = __builtin_amdgcn_readlane(my_at, holder);
+    len = __builtin_amdgcn_readlane(my_len, holder);
+  }
   bool first_segment = true;
 
   while (left > 0) {
@@ -486,7 +504,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(Decod
       }
     }
     __syncthreads();
-    const bool done = u0 == 0 && n == row_units;  // the whole row
+    const bool done = WHOLE || (u0 == 0 && n == row_units);  // the whole row
     const long long slot = 2ll * blockIdx.x + (first_segment ? 0 : 1);
     const int rows = min(RT * kRows, heads);
     constexpr int kLanes = kHeadDim / 4;  // threads of a head, four elements each
@@ -531,6 +549,7 @@ struct Parts {
 
 // The parts of sequence b's row (key head and tile of heads). Every wave for itself.
 __device__ __forceinline__ Parts parts_of(const DecodeParams& p, int b, int row) {
+  if (p.most_workers == 0) return Parts{0, 0, 0};
   int all = 0, before = 0;
   for (int i = threadIdx.x % kWave; i < p.batch; i += kWave) {
     const int u = units_of(p, i);
@@ -686,7 +705,7 @@ __device__ __forceinline__ void add_weights(const DecodeParams& p, int chunk, in
 // The first batch * hq workgroups join a head each; the others add the weights.
 __global__ __launch_bounds__(kJoin) void decode_join(DecodeParams p, int chunks,
                                                         float* __restrict__ weights) {
-  const int heads = p.batch * p.hq, i = blockIdx.x;
+  const int heads = p.most_workers ? p.batch * p.hq : 0, i = blockIdx.x;
   if (i < heads)
     join(p, i);
   else
@@ -706,12 +725,29 @@ int tile_rows_of(int group) {
   return group < 2 * kRows ? group : 2 * kRows;
 }
 
-Scratch scratch_of(const CacheParams& c, int batch, int hq, bool weights) {
-  const size_t rows = 2 * (size_t)kMostWorkers * tile_rows_of(hq / c.hkv);
+// Whether every row is one workgroup's: where rows are short, or not long and either
+// many or e4m3 (half the bytes a key). Then there are no parts and no join, and a
+// workspace only for weights. In us, shares and join / whole rows, 32 / 8 heads unless
+// noted, of up to as many keys as the table holds:
+//    512 keys  1 sequence 10.2 / 7.8, e4m3 9.7 / 7.0; 64 24.3 / 17.7, 18.2 / 11.7;
+//              256 71.5 / 55.5, 43.9 / 29.1
+//   1024 keys  1 sequence 10.4 / 12.3, e4m3 9.8 / 9.3; 8 12.3 / 14.4, 11.7 / 10.7;
+//              64 31.8 / 29.6, 23.0 / 18.0; 256 114 / 99, 69 / 53; 64 of 40 / 2 heads
+//              23.5 / 15.7, 20.4 / 14.0; 32 of 24 / 24 heads 41.3 / 43.0, 27.5 / 25.3
+//   2048 keys  1 sequence 10.9 / 22.8, e4m3 10.3 / 17.8; 64 53.4 / 54.1, 34.6 / 30.1;
+//              32 of 24 / 24 heads 80.6 / 92.9, 43.9 / 46.0
+bool whole_rows(const CacheParams& c, bool e4m3, int rows) {
+  return c.capacity() <= 512 || (c.capacity() <= 1024 && (e4m3 || rows >= 128));
+}
+
+Scratch scratch_of(const CacheParams& c, bool e4m3, int batch, int hq, bool weights) {
+  const int group = hq / c.hkv, tile_rows = tile_rows_of(group);
+  const int rows = batch * c.hkv * ((group + tile_rows - 1) / tile_rows);
+  const size_t parts = whole_rows(c, e4m3, rows) ? 0 : 2 * (size_t)kMostWorkers * tile_rows;
   Scratch s;
   s.part = 0;
-  s.ml = s.part + align256(rows * kHeadDim * 4);
-  s.stat = s.ml + align256(rows * 8);
+  s.ml = s.part + align256(parts * kHeadDim * 4);
+  s.stat = s.ml + align256(parts * 8);
   s.z = s.stat + (weights ? align256((size_t)batch * hq * 8) : 0);
   s.bytes = s.z + (weights ? align256((size_t)batch * hq * c.capacity() * 4) : 0);
   return s;
@@ -719,14 +755,14 @@ Scratch scratch_of(const CacheParams& c, int batch, int hq, bool weights) {
 
 }  // namespace
 
-size_t decode_scratch_bytes(const CacheParams& c, int batch, int hq, bool weights) {
-  return scratch_of(c, batch, hq, weights).bytes;
+size_t decode_scratch_bytes(const CacheParams& c, bool e4m3, int batch, int hq, bool weights) {
+  return scratch_of(c, e4m3, batch, hq, weights).bytes;
 }
 
 hipError_t launch_decode(const void* q, const CacheParams& c, bool e4m3, int batch, int hq,
                          const int32_t* lens, void* o, float* lse, float* weights, void* scratch,
                          hipStream_t st) {
-  const Scratch s = scratch_of(c, batch, hq, weights != nullptr);
+  const Scratch s = scratch_of(c, e4m3, batch, hq, weights != nullptr);
   DecodeParams p;
   p.c = c;
   p.q = (const uint16_t*)q;
@@ -742,18 +778,24 @@ hipError_t launch_decode(const void* q, const CacheParams& c, bool e4m3, int bat
   p.ml = (float*)((char*)scratch + s.ml);
   p.stat = weights ? (float*)((char*)scratch + s.stat) : nullptr;
   p.z = weights ? (float*)((char*)scratch + s.z) : nullptr;
-  // no more workgroups than there can be shares
   const int rows = batch * c.hkv * p.row_tiles;
+  const bool whole = whole_rows(c, e4m3, rows);
+  // no more workgroups than there can be shares
   const long long units = (long long)rows * ((c.capacity() + kUnit - 1) / kUnit);
-  p.most_workers = most_workers(rows);
+  p.most_workers = whole ? 0 : most_workers(rows);
   if ((units + 1) / 2 < p.most_workers) p.most_workers = (int)((units + 1) / 2);
-  auto* kernel = p.tile_rows <= kRows ? (e4m3 ? decode_kernel<true, 1> : decode_kernel<false, 1>)
-                                      : (e4m3 ? decode_kernel<true, 2> : decode_kernel<false, 2>);
-  hipLaunchKernelGGL(kernel, dim3(p.most_workers), dim3(kThreads), 0, st, p);
+  void (*const kernels[2][2][2])(DecodeParams) = {
+      {{decode_kernel<false, 1, false>, decode_kernel<false, 1, true>},
+       {decode_kernel<false, 2, false>, decode_kernel<false, 2, true>}},
+      {{decode_kernel<true, 1, false>, decode_kernel<true, 1, true>},
+       {decode_kernel<true, 2, false>, decode_kernel<true, 2, true>}}};
+  hipLaunchKernelGGL(kernels[e4m3][p.tile_rows > kRows][whole],
+                     dim3((unsigned)(whole ? rows : p.most_workers)), dim3(kThreads), 0, st, p);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || (whole && !weights)) return e;
   const int chunks = weights ? (c.capacity() + kWeightKeys - 1) / kWeightKeys : 0;
-  hipLaunchKernelGGL(decode_join, dim3((unsigned)(batch * (hq + c.hkv * chunks))), dim3(kJoin),
-                     0, st, p, chunks, weights);
+  const int heads = whole ? 0 : batch * hq;
+  hipLaunchKernelGGL(decode_join, dim3((unsigned)(heads + batch * c.hkv * chunks)), dim3(kJoin), 0,
+                     st, p, chunks, weights);
   return hipGetLastError();
 }

@@ -135,6 +135,13 @@ int check_cache_arrays(const xattn_cache* c, const int32_t* table) {
   return XATTN_OK;
 }
 
+int check_workspace(const void* workspace, size_t bytes, size_t need) {
+  if (need && (!workspace || bytes < need || (uintptr_t)workspace % 16 != 0))
+    return fail(XATTN_ERR_WORKSPACE, "a 16-byte aligned workspace of %zu bytes needed, %zu given",
+                need, workspace ? bytes : (size_t)0);
+  return XATTN_OK;
+}
+
 int check_decode(const xattn_cache* cache, int batch, int hq, const int32_t* table,
                  int table_pages, CacheParams* c) {
   int rc;
@@ -218,7 +225,7 @@ int xattn_decode_workspace_size(const xattn_cache* cache, int batch, int hq, int
   CacheParams c;
   if ((rc = check_decode(cache, batch, hq, nullptr, table_pages, &c))) return rc;
   if (!bytes) return fail(XATTN_ERR_ARG, "bytes is NULL");
-  *bytes = decode_scratch_bytes(c, batch, hq, weights != 0);
+  *bytes = decode_scratch_bytes(c, cache->type == XATTN_CACHE_E4M3, batch, hq, weights != 0);
   return ok();
 }
 
@@ -232,12 +239,11 @@ int xattn_decode(const void* q, const xattn_cache* cache, int batch, int hq,
       (rc = check_pointer(lens, "lens", 4)) || (rc = check_cache_arrays(cache, table)) ||
       (weights && (rc = check_pointer(weights, "weights", 16))))
     return rc;
-  const size_t need = decode_scratch_bytes(c, batch, hq, weights != nullptr);
-  if (!workspace || workspace_bytes < need || (uintptr_t)workspace % 16 != 0)
-    return fail(XATTN_ERR_WORKSPACE, "a 16-byte aligned workspace of %zu bytes needed, %zu given",
-                need, workspace ? workspace_bytes : (size_t)0);
-  return launched(launch_decode(q, c, cache->type == XATTN_CACHE_E4M3, batch, hq, lens, o, lse,
-                                weights, workspace, (hipStream_t)stream),
+  const bool e4m3 = cache->type == XATTN_CACHE_E4M3;
+  const size_t need = decode_scratch_bytes(c, e4m3, batch, hq, weights != nullptr);
+  if ((rc = check_workspace(workspace, workspace_bytes, need))) return rc;
+  return launched(launch_decode(q, c, e4m3, batch, hq, lens, o, lse, weights, workspace,
+                                (hipStream_t)stream),
                   "xattn_decode");
 }
 
@@ -275,9 +281,7 @@ int xattn_cache_evict(const xattn_cache* cache, int batch, const int32_t* table,
   if (new_lens == lens || new_weights == weights || new_table == table)
     return fail(XATTN_ERR_ARG, "an output is its own input, or new_table is table");
   const size_t need = evict_scratch_bytes(c, batch);
-  if (need && (!workspace || workspace_bytes < need || (uintptr_t)workspace % 16 != 0))
-    return fail(XATTN_ERR_WORKSPACE, "a 16-byte aligned workspace of %zu bytes needed, %zu given",
-                need, workspace ? workspace_bytes : (size_t)0);
+  if ((rc = check_workspace(workspace, workspace_bytes, need))) return rc;
   return launched(launch_evict(c, cache->type == XATTN_CACHE_E4M3, batch, lens, weights, budget,
                                recent, new_table, new_pages, kept, new_lens, new_weights,
                                workspace, (hipStream_t)stream),

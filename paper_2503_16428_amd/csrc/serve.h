@@ -57,7 +57,8 @@ hipError_t launch_append(const void* k, const xattn::Strides& ks, const void* v,
                          const int32_t* start, const int32_t* pos,
                          const xattn::RotaryParams* plan, bool interleaved,
                          const xattn::CacheParams& c, bool e4m3, hipStream_t st);
-size_t decode_scratch_bytes(const xattn::CacheParams& c, int batch, int hq, bool weights);
+size_t decode_scratch_bytes(const xattn::CacheParams& c, bool e4m3, int batch, int hq,
+                            bool weights);
 hipError_t launch_decode(const void* q, const xattn::CacheParams& c, bool e4m3, int batch, int hq,
                          const int32_t* lens, void* o, float* lse, float* weights, void* scratch,
                          hipStream_t st);

@@ -244,9 +244,9 @@ def xattn_cache_append(k, v, cache: KVCache, table, start, count=None, pos=None,
 
 
 @functools.lru_cache(maxsize=256)
-def _decode_bytes(hkv, page, batch, hq, table_pages, weights):
+def _decode_bytes(hkv, page, e4m3, batch, hq, table_pages, weights):
     """Workspace bytes of a shape; a function of the shape alone."""
-    c = Cache(1, page, hkv, HEAD_DIM, 0, None, None, None, None)
+    c = Cache(1, page, hkv, HEAD_DIM, int(e4m3), None, None, None, None)
     n = ctypes.c_size_t(0)
     _check(lib().xattn_decode_workspace_size(ctypes.byref(c), batch, hq, table_pages, weights,
                                              ctypes.byref(n)))
@@ -257,7 +257,7 @@ def decode_workspace_size(cache: KVCache, batch: int, hq: int, table_pages: int,
                           weights: bool = False) -> int:
     """Bytes of xattn_decode's workspace."""
     _is_cache(cache)
-    return _decode_bytes(cache.hkv, cache.page, int(batch), int(hq), int(table_pages),
+    return _decode_bytes(cache.hkv, cache.page, cache.e4m3, int(batch), int(hq), int(table_pages),
                          int(bool(weights)))
 
 
@@ -283,16 +283,16 @@ def xattn_decode(q, cache: KVCache, table, lens, o=None, lse=None, weights=None,
     at = _here(q, (table, lens, cache.k, o, lse, weights, workspace),
                ("q", "table", "lens", "cache", "o", "lse", "weights", "workspace"), dense)
     def allocate():
-        need = 0 if workspace is not None else _decode_bytes(cache.hkv, cache.page, b, hq, width,
-                                                             int(weights is not None))
+        need = 0 if workspace is not None else _decode_bytes(
+            cache.hkv, cache.page, cache.e4m3, b, hq, width, int(weights is not None))
         return (q.new_empty(shape) if o is None else o,
                 q.new_empty((b, hq), dtype=torch.float32) if lse is None and want_lse else lse,
-                q.new_empty((need,), dtype=torch.uint8) if workspace is None else workspace)
+                q.new_empty((need,), dtype=torch.uint8) if need else workspace)
 
     o, lse, workspace = _made(stream, allocate)
     _check(lib().xattn_decode(q.data_ptr(), cache._ref, b, hq, table.data_ptr(), width,
                               lens.data_ptr(), o.data_ptr(), _ptr(lse), _ptr(weights),
-                              workspace.data_ptr(), workspace.numel(),
+                              _ptr(workspace), 0 if workspace is None else workspace.numel(),
                               _handle(stream, at)))
     return o, lse
 

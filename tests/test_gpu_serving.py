@@ -270,8 +270,12 @@ def test_append_in_8_bits_at_the_ends_of_the_range(rotated):
 # ---- decode
 
 
-def decode_case(batch, hq, hkv, page, lens, e4m3, seed=30, columns=None, spare=2):
+def decode_case(batch, hq, hkv, page, lens, e4m3, seed=30, columns=None, spare=2, wide=False):
+    """wide: a table of more than 1024 tokens, whose rows are shared out among workgroups; short
+    ones are one workgroup's each."""
     columns = columns or max(1, -(-max(lens) // page)) + 1
+    if wide:
+        columns = max(columns, 1040 // page + 1)
     pages = batch * columns + spare
     g = gen(seed)
     k = torch.randn((pages, hkv, page, 128), generator=g) * 1.3
@@ -319,18 +323,29 @@ def check_decode(q, k, v, scales, table, lens, weights=True):
     return o, lse, w
 
 
+WIDE = pytest.mark.parametrize("wide", [False, True])
+
+
+@WIDE
 @pytest.mark.parametrize("e4m3", [False, True])
 @pytest.mark.parametrize("hq,hkv", [(1, 1), (4, 1), (7, 1), (16, 1), (17, 1), (40, 1), (6, 3), (8, 8)])
-def test_decode_heads(hq, hkv, e4m3):
+def test_decode_heads(hq, hkv, e4m3, wide):
     lens = [77, 1, 300]
-    check_decode(*decode_case(3, hq, hkv, 16, lens, e4m3), lens)
+    check_decode(*decode_case(3, hq, hkv, 16, lens, e4m3, wide=wide), lens)
 
 
+@WIDE
 @pytest.mark.parametrize("e4m3", [False, True])
 @pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
-def test_decode_lengths(page, e4m3):
+def test_decode_lengths(page, e4m3, wide):
     lens = [0, 1, 2, 15, 16, 17, 31, 33, 63, 64, 65, 127, 129, page, page + 1, 2 * page - 1]
-    check_decode(*decode_case(len(lens), 4, 2, page, lens, e4m3), lens)
+    check_decode(*decode_case(len(lens), 4, 2, page, lens, e4m3, wide=wide), lens)
+
+
+@WIDE
+def test_decode_without_keys(wide):
+    for lens in ([0], [0, 0, 0]):
+        check_decode(*decode_case(len(lens), 40, 2, 16, lens, False, wide=wide), lens)
 
 
 @pytest.mark.parametrize("e4m3", [False, True])
@@ -340,14 +355,25 @@ def test_decode_long(hq, hkv, lens, page, e4m3):
     check_decode(*decode_case(len(lens), hq, hkv, page, lens, e4m3), lens)
 
 
-def test_decode_of_many_short_sequences():
+@WIDE
+def test_decode_of_many_short_sequences(wide):
     lens = [(37 * i) % 90 for i in range(150)]
-    check_decode(*decode_case(150, 4, 1, 16, lens, False), lens)
+    check_decode(*decode_case(150, 4, 1, 16, lens, False, wide=wide), lens)
 
 
-def test_decode_of_more_sequences_than_lanes():
+@pytest.mark.parametrize("columns", [32, 33, 64, 65])
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_decode_around_the_lengths_of_whole_rows(columns, e4m3):
+    """Tables of 512, 528, 1024 and 1040 tokens, few rows and many."""
+    for batch in (2, 64):
+        lens = [columns * 16 - (13 * i) % (columns * 16) for i in range(batch)]
+        check_decode(*decode_case(batch, 4, 2, 16, lens, e4m3, columns=columns), lens)
+
+
+@pytest.mark.parametrize("columns", [13, 66])
+def test_decode_of_more_sequences_than_lanes(columns):
     lens = [(7 * i) % 5 if i % 97 else 200 for i in range(1000)]
-    check_decode(*decode_case(1000, 1, 1, 16, lens, False, spare=0, columns=13), lens)
+    check_decode(*decode_case(1000, 1, 1, 16, lens, False, spare=0, columns=columns), lens)
 
 
 @pytest.mark.parametrize("seed", range(24))
@@ -374,10 +400,11 @@ def test_decode_of_lengths_past_the_table():
     assert all(torch.equal(bits(x), bits(y)) for x, y in zip(a, b))
 
 
+@WIDE
 @pytest.mark.parametrize("e4m3", [False, True])
-def test_what_lies_behind_a_length_has_no_effect(e4m3):
+def test_what_lies_behind_a_length_has_no_effect(e4m3, wide):
     lens = [5, 0, 83, 64]
-    q, k, v, s, table = decode_case(4, 4, 2, 32, lens, e4m3)
+    q, k, v, s, table = decode_case(4, 4, 2, 32, lens, e4m3, wide=wide)
     clean = check_decode(q, k, v, s, table, lens)
     used = torch.zeros(k.shape[0], k.shape[2], dtype=torch.bool)
     for b, n in enumerate(lens):
@@ -400,19 +427,21 @@ def test_what_lies_behind_a_length_has_no_effect(e4m3):
         assert torch.equal(bits(dirty[1]), bits(clean[1]))
 
 
+@WIDE
 @pytest.mark.parametrize("e4m3", [False, True])
-def test_decode_skips_missing_pages(e4m3):
+def test_decode_skips_missing_pages(e4m3, wide):
     lens = [100, 64, 40]
-    q, k, v, s, table = decode_case(3, 4, 2, 16, lens, e4m3)
+    q, k, v, s, table = decode_case(3, 4, 2, 16, lens, e4m3, wide=wide)
     table[0, 1], table[0, 5] = -1, k.shape[0]
     table[1, :] = -2**31          # a row without a key
     table[2, 0] = 2**31 - 1
     check_decode(q, k, v, s, table, lens)
 
 
-def test_products_of_minus_infinity_have_no_weight():
+@WIDE
+def test_products_of_minus_infinity_have_no_weight(wide):
     lens = [40, 20]
-    q, k, v, s, table = decode_case(2, 4, 1, 16, lens, False)
+    q, k, v, s, table = decode_case(2, 4, 1, 16, lens, False, wide=wide)
     q = q.abs() + 0.5
     k[table[0, 0], :, :] = -INF                  # the first sequence's first page
     v[table[0, 0], 0, 3] = 7.0
@@ -420,9 +449,10 @@ def test_products_of_minus_infinity_have_no_weight():
     check_decode(q, k, v, s, table, lens)
 
 
-def test_infinite_and_nan_products_reach_their_own_row_only():
+@WIDE
+def test_infinite_and_nan_products_reach_their_own_row_only(wide):
     lens = [40, 40, 40]
-    q, k, v, s, table = decode_case(3, 4, 1, 16, lens, False)
+    q, k, v, s, table = decode_case(3, 4, 1, 16, lens, False, wide=wide)
     clean = X.xattn_decode(q.cuda(), on_gpu(k, v, s), table.cuda(), ints(lens), want_lse=True)
     k[table[1, 1], 0, 4] = NAN
     v[table[2, 0], 0, 5, 9] = INF
@@ -434,10 +464,11 @@ def test_infinite_and_nan_products_reach_their_own_row_only():
     assert torch.equal(bits(o[2].cpu()[:, rest]), bits(clean[0][2].cpu()[:, rest]))
 
 
-def test_large_products_and_weights_of_one_key():
+@WIDE
+def test_large_products_and_weights_of_one_key(wide):
     """One key far above the rest, late and early, and keys alike."""
     lens = [300, 300, 33]
-    q, k, v, s, table = decode_case(3, 4, 2, 64, lens, False)
+    q, k, v, s, table = decode_case(3, 4, 2, 64, lens, False, wide=wide)
     q[0], q[1] = q[0].abs() * 4, q[1].abs() * 4
     k[table[0, 4], :, 20] = 30.0
     k[table[1, 0], :, 0] = 30.0

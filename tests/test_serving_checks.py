@@ -122,9 +122,13 @@ def test_decode_refuses(kw):
 def test_decode_refuses_workspaces_and_sizes():
     n = ctypes.c_size_t(0)
     c = c_cache()
-    assert X.lib().xattn_decode_workspace_size(c, 1, 4, 2, 0, ctypes.byref(n)) == 0
+    assert X.lib().xattn_decode_workspace_size(c, 1, 4, 200, 0, ctypes.byref(n)) == 0
+    assert n.value > 0
     for kw in (dict(ws=None), dict(bytes=n.value - 1), dict(ws=FAKE + 8)):
-        refused(decode(**kw), B.XATTN_ERR_WORKSPACE)
+        refused(decode(pages=200, **kw), B.XATTN_ERR_WORKSPACE)
+    assert X.lib().xattn_decode_workspace_size(c, 1, 4, 2, 0, ctypes.byref(n)) == 0
+    assert n.value == 0  # a row is one workgroup's; with weights its products are kept
+    refused(decode(weights=FAKE, ws=None), B.XATTN_ERR_WORKSPACE)
     refused(X.lib().xattn_decode_workspace_size(c, 1, 4, 2, 0, None))
     refused(X.lib().xattn_decode_workspace_size(c, 1, 3, 2, 0, ctypes.byref(n)))
     U = B.XATTN_ERR_UNSUPPORTED
@@ -145,10 +149,10 @@ def test_decode_workspaces_grow_with_the_call():
 
     for batch, hq, pages in ((1, 2, 1), (3, 34, 7), (64, 32, 1000), (1, 64, 8192)):
         plain = size(batch, hq, pages, 0)
-        assert 0 < plain < 1 << 34
+        assert (0 < plain < 1 << 34) if pages > 64 else plain == 0
         # the products of every head and token, for the weights
         assert size(batch, hq, pages, 1) >= plain + batch * hq * pages * 16 * 4
-        assert size(batch, hq, pages, 0, type=1, k_scale=FAKE, v_scale=FAKE) > 0
+        assert size(batch, hq, pages, 0, type=1, k_scale=FAKE, v_scale=FAKE) == plain
 
 
 def evict(**kw):
