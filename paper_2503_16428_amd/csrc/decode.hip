@@ -731,13 +731,16 @@ int tile_rows_of(int group) {
 // noted, of up to as many keys as the table holds:
 //    512 keys  1 sequence 10.2 / 7.8, e4m3 9.7 / 7.0; 64 24.3 / 17.7, 18.2 / 11.7;
 //              256 71.5 / 55.5, 43.9 / 29.1
+//    640 keys  1 sequence 11.4 / 9.1, 8 12.4 / 10.0, 1 of 4 / 1 heads 10.2 / 9.6
+//    768 keys  1 sequence 10.6 / 10.3, 8 12.3 / 11.5, 1 of 4 / 1 heads 10.0 / 10.9
+//    896 keys  1 sequence 11.7 / 11.5, 8 12.4 / 13.0, 1 of 4 / 1 heads 9.9 / 12.2
 //   1024 keys  1 sequence 10.4 / 12.3, e4m3 9.8 / 9.3; 8 12.3 / 14.4, 11.7 / 10.7;
 //              64 31.8 / 29.6, 23.0 / 18.0; 256 114 / 99, 69 / 53; 64 of 40 / 2 heads
 //              23.5 / 15.7, 20.4 / 14.0; 32 of 24 / 24 heads 41.3 / 43.0, 27.5 / 25.3
 //   2048 keys  1 sequence 10.9 / 22.8, e4m3 10.3 / 17.8; 64 53.4 / 54.1, 34.6 / 30.1;
 //              32 of 24 / 24 heads 80.6 / 92.9, 43.9 / 46.0
 bool whole_rows(const CacheParams& c, bool e4m3, int rows) {
-  return c.capacity() <= 512 || (c.capacity() <= 1024 && (e4m3 || rows >= 128));
+  return c.capacity() <= 768 || (c.capacity() <= 1024 && (e4m3 || rows >= 128));
 }
 
 Scratch scratch_of(const CacheParams& c, bool e4m3, int batch, int hq, bool weights) {

@@ -361,10 +361,10 @@ def test_decode_of_many_short_sequences(wide):
     check_decode(*decode_case(150, 4, 1, 16, lens, False, wide=wide), lens)
 
 
-@pytest.mark.parametrize("columns", [32, 33, 64, 65])
+@pytest.mark.parametrize("columns", [32, 33, 48, 49, 64, 65])
 @pytest.mark.parametrize("e4m3", [False, True])
 def test_decode_around_the_lengths_of_whole_rows(columns, e4m3):
-    """Tables of 512, 528, 1024 and 1040 tokens, few rows and many."""
+    """Tables of 512, 768, 1024 and a page more tokens, few rows and many."""
     for batch in (2, 64):
         lens = [columns * 16 - (13 * i) % (columns * 16) for i in range(batch)]
         check_decode(*decode_case(batch, 4, 2, 16, lens, e4m3, columns=columns), lens)
