@@ -318,8 +318,9 @@ int xattn_head_error_mean(const void *o, const void *o_ref, const xattn_dims *di
  * Strides: `x_strides` holds 3 host int64, the distances in ELEMENTS between
  * batch elements, heads and tokens of x[batch][heads][tokens][128]; the 128
  * values of a vector are contiguous. Strides are >= 0 and multiples of 8 (the
- * stride of a dimension of size 1 is not used); every array of bfloat16 or
- * cache values is 16-byte aligned. Read during the call only.
+ * stride of a dimension of size 1 is not used), those of an output from the smallest
+ * on at least what the smaller ones span, so that no two vectors overlap; every
+ * array of bfloat16 or cache values is 16-byte aligned. Read during the call only.
  */
 
 /* Rotary positions: the 64 pairs of a head are shared out among `axes` position

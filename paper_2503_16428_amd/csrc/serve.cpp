@@ -2,7 +2,7 @@
 // workspace sizing. Declarations and contracts are in include/xattn.h.
 #include <hip/hip_runtime.h>
 
-#include <cmath>
+#include <algorithm>
 
 #include "serve.h"
 #include "xattn.h"
@@ -29,14 +29,20 @@ int launched(hipError_t e, const char* what) {
   return ok();
 }
 
-int check_pointer(const void* p, const char* name, size_t align) {
-  if (!p) return fail(XATTN_ERR_ARG, "%s must be non-NULL", name);
+int check_aligned(const void* p, const char* name, size_t align) {
   if ((uintptr_t)p % align != 0)
     return fail(XATTN_ERR_ARG, "%s must be aligned to %zu bytes", name, align);
   return XATTN_OK;
 }
 
-// Strides of [batch][heads][tokens] vectors; of a dimension of size 1 unused.
+int check_pointer(const void* p, const char* name, size_t align) {
+  if (!p) return fail(XATTN_ERR_ARG, "%s must be non-NULL", name);
+  return check_aligned(p, name, align);
+}
+
+// Strides of [batch][heads][tokens] vectors; of a dimension of size 1 unused. Those
+// of an output keep its vectors apart: from the smallest on, each passes all that
+// the ones before it span.
 int check_strides(const int64_t* s, const char* name, int batch, int heads, int tokens,
                   bool written, Strides* out) {
   if (!s) return fail(XATTN_ERR_ARG, "the strides of %s are NULL", name);
@@ -47,9 +53,18 @@ int check_strides(const int64_t* s, const char* name, int batch, int heads, int 
     if (v[i] < 0 || v[i] % 8 != 0 || v[i] > (1ll << 40))
       return fail(XATTN_ERR_ARG, "stride %d of %s must be a multiple of 8 from 0 to 2^40 (got %lld)",
                   i, name, (long long)s[i]);
-    if (written && size[i] > 1 && v[i] < xattn::kHeadDim)
-      return fail(XATTN_ERR_ARG, "stride %d of the output %s lets its vectors overlap (%lld)", i,
-                  name, (long long)s[i]);
+  }
+  if (written) {
+    int by_stride[3] = {0, 1, 2};
+    std::sort(by_stride, by_stride + 3, [&](int a, int b) { return v[a] < v[b]; });
+    double span = xattn::kHeadDim;  // elements; a sum may pass 64 bits
+    for (int i : by_stride) {
+      if (size[i] == 1) continue;
+      if ((double)v[i] < span)
+        return fail(XATTN_ERR_ARG, "stride %d of the output %s lets its vectors overlap (%lld)", i,
+                    name, (long long)s[i]);
+      span += (double)v[i] * (size[i] - 1);
+    }
   }
   *out = Strides{v[0], v[1], v[2]};
   return XATTN_OK;
@@ -211,7 +226,8 @@ int xattn_cache_append(const void* k, const int64_t* k_strides, const void* v,
       (rc = check_strides(k_strides, "k", batch, cache->hkv, tokens, false, &ks)) ||
       (rc = check_strides(v_strides, "v", batch, cache->hkv, tokens, false, &vs)) ||
       (rc = check_pointer(k, "k", 16)) || (rc = check_pointer(v, "v", 16)) ||
-      (rc = check_pointer(start, "start", 4)) || (rc = check_cache_arrays(cache, table)))
+      (rc = check_pointer(start, "start", 4)) || (rc = check_aligned(count, "count", 4)) ||
+      (rc = check_aligned(pos, "pos", 4)) || (rc = check_cache_arrays(cache, table)))
     return rc;
   return launched(launch_append(k, ks, v, vs, batch, tokens, count, start, pos,
                                 plan ? &p : nullptr, plan && plan->interleaved, c,
@@ -237,7 +253,7 @@ int xattn_decode(const void* q, const xattn_cache* cache, int batch, int hq,
   if ((rc = check_decode(cache, batch, hq, table, table_pages, &c)) ||
       (rc = check_pointer(q, "q", 16)) || (rc = check_pointer(o, "o", 16)) ||
       (rc = check_pointer(lens, "lens", 4)) || (rc = check_cache_arrays(cache, table)) ||
-      (weights && (rc = check_pointer(weights, "weights", 16))))
+      (rc = check_aligned(lse, "lse", 4)) || (rc = check_aligned(weights, "weights", 16)))
     return rc;
   const bool e4m3 = cache->type == XATTN_CACHE_E4M3;
   const size_t need = decode_scratch_bytes(c, e4m3, batch, hq, weights != nullptr);

@@ -63,6 +63,8 @@ def rotary(**kw):
     dict(heads=0), dict(tokens=-1), dict(dim=0), dict(inverse=2),
     dict(xs=strides(0, 4, 256)), dict(xs=strides(0, -128, 256)), dict(xs=strides(0, 128, 2**41)),
     dict(os=strides(0, 384, 0)), dict(os=strides(0, 0, 128)), dict(os=strides(0, 384, 64)),
+    dict(os=strides(0, 128, 128)), dict(os=strides(0, 256, 128)), dict(os=strides(0, 128, 248)),
+    dict(batch=2, os=strides(128, 384, 128)), dict(batch=2, os=strides(640, 384, 128)),
     dict(plan=c_plan(axes=0)), dict(plan=c_plan(axes=4)), dict(plan=c_plan(pairs=(0, 0, 0))),
     dict(plan=c_plan(pairs=(60, 4, 0))), dict(plan=c_plan(axes=2, pairs=(60, 5, 0))),
     dict(plan=c_plan(axes=2, pairs=(60, 0, 0))), dict(plan=c_plan(pairs=(65, 0, 0))),
@@ -96,6 +98,7 @@ BAD_CACHES = [dict(page=0), dict(page=8), dict(page=48), dict(page=512), dict(pa
 @pytest.mark.parametrize("kw", [
     dict(k=None), dict(v=None), dict(v=FAKE + 4), dict(ks=None), dict(vs=strides(0, 128, 12)),
     dict(batch=0), dict(tokens=0), dict(start=None), dict(table=None), dict(pages=0),
+    dict(count=FAKE + 2), dict(pos=FAKE + 1, plan=c_plan()),
     dict(pos=FAKE), dict(plan=c_plan()), dict(pos=FAKE, plan=c_plan(axes=5)), dict(cache=None),
     *[dict(cache=c_cache(**c)) for c in BAD_CACHES]])
 def test_append_refuses(kw):
@@ -104,16 +107,16 @@ def test_append_refuses(kw):
 
 def decode(**kw):
     d = dict(q=FAKE, cache=c_cache(), batch=1, hq=4, table=FAKE, pages=2, lens=FAKE, o=FAKE,
-             weights=None, ws=FAKE, bytes=1 << 40)
+             weights=None, lse=None, ws=FAKE, bytes=1 << 40)
     d.update(kw)
     return X.lib().xattn_decode(d["q"], d["cache"], d["batch"], d["hq"], d["table"], d["pages"],
-                                d["lens"], d["o"], None, d["weights"], d["ws"], d["bytes"], None)
+                                d["lens"], d["o"], d["lse"], d["weights"], d["ws"], d["bytes"], None)
 
 
 @pytest.mark.parametrize("kw", [
     dict(q=None), dict(q=FAKE + 8), dict(o=None), dict(lens=None), dict(table=None), dict(batch=0),
     dict(hq=0), dict(hq=3), dict(pages=0), dict(pages=-1), dict(cache=None),
-    dict(weights=FAKE + 4),
+    dict(weights=FAKE + 4), dict(lse=FAKE + 2),
     *[dict(cache=c_cache(**c)) for c in BAD_CACHES]])
 def test_decode_refuses(kw):
     refused(decode(**kw))
