@@ -415,9 +415,8 @@ int xattn_cache_append(const void *k, const int64_t *k_strides, const void *v,
  *   lens     int32 [batch] device
  *   lse      fp32 [batch][hq] (output) or NULL
  *   weights  fp32 [batch][hkv][table_pages * page], 16-byte aligned (updated), or
- *            NULL: entry t of
- *            a key head grows by the sum of its query heads' softmax_t, for
- *            t < lens[b]; what lies behind is left as it was
+ *            NULL: entry t of a key head grows by the sum of its query heads'
+ *            softmax_t, for t < lens[b]; what lies behind is left as it was
  *   workspace  at least xattn_decode_workspace_size() bytes (`weights`: whether
  *            the call has them; 0 for small calls, then it may be NULL), 16-byte
  *            aligned; its contents on entry are ignored. Calls that may run at the
@@ -453,8 +452,12 @@ int xattn_decode(const void *q, const xattn_cache *cache, int batch, int hq,
  *                weights, 0 behind them; no memory of weights
  *   workspace    as for xattn_decode, xattn_evict_workspace_size() bytes (0 for
  *                rows of up to 16384 tokens, then it may be NULL)
- * The weights are 16-byte aligned. 1 <= budget, 0 <= recent <= budget. Page rows behind the kept tokens are left
- * as they were.
+ * The weights are 16-byte aligned. 1 <= budget, 0 <= recent <= budget. Page rows
+ * behind the kept tokens are left as they were. A token without a page takes its
+ * place among the kept ones like any other, by its weight, and there is nothing to
+ * move: that place is left as it was too, and a later call attends to it. So every
+ * token below lens that can be kept should have a page (a weight of NaN is below all
+ * others, where those fill the budget).
  */
 int xattn_evict_workspace_size(const xattn_cache *cache, int batch, int table_pages, size_t *bytes);
 int xattn_cache_evict(const xattn_cache *cache, int batch, const int32_t *table, int table_pages,

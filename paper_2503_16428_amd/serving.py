@@ -315,7 +315,8 @@ def evict_workspace_size(cache: KVCache, batch: int, table_pages: int) -> int:
 def xattn_cache_evict(cache: KVCache, table, lens, weights, new_table, budget: int, recent: int,
                       kept=None, new_lens=None, new_weights=None, workspace=None, stream=None):
     """Moves the `budget` most valuable tokens of every sequence and key head (the last `recent`
-    and the heaviest before them) to the pages of new_table, none of which is in table. Returns
+    and the heaviest before them) to the pages of new_table, none of which is in table. Tokens that
+    can be kept need a page: of others the new place is left as it was. Returns
     (kept int32 [batch, hkv, budget], new_lens int32 [batch], new_weights fp32 [batch, hkv,
     new_pages * page])."""
     _is_cache(cache)

@@ -706,19 +706,21 @@ def test_evict_with_missing_pages():
 # ---- together
 
 
-def test_graph_of_a_decoding_step_replays_like_eager():
+@pytest.mark.parametrize("columns", [8, 66])
+def test_graph_of_a_decoding_step_replays_like_eager(columns):
     """Rotation, append, attention with weights and eviction in one captured step, on new inputs
-    and lengths at every replay; two graphs share a workspace."""
+    and lengths at every replay; two graphs share a workspace. Rows of one workgroup, and shared
+    ones."""
     batch, hq, hkv, page = 3, 8, 2, 16
     lens = [60, 33, 0]
-    q, k, v, s, table = decode_case(batch, hq, hkv, page, lens, False, columns=8, spare=40)
+    q, k, v, s, table = decode_case(batch, hq, hkv, page, lens, False, columns=columns, spare=40)
     plan = X.Rotary([64], R.freqs([64]))
     free = [p for p in range(k.shape[0]) if p not in table.flatten().tolist()]
     new_table = torch.tensor(free[:batch * 2]).view(batch, 2).int().cuda()
     td = table.cuda()
 
     def fresh():
-        return on_gpu(k, v, s), torch.zeros((batch, hkv, 8 * page), device="cuda")
+        return on_gpu(k, v, s), torch.zeros((batch, hkv, columns * page), device="cuda")
 
     def step(cache, w, x, key, value, pos, start, ln, ws):
         X.xattn_rotary(x, pos, plan, out=x)
@@ -734,7 +736,7 @@ def test_graph_of_a_decoding_step_replays_like_eager():
                     ln=ints([n + i + 1 for n in lens]))
 
     probe, _ = fresh()
-    ws = torch.empty(X.decode_workspace_size(probe, batch, hq, 8, True), dtype=torch.uint8,
+    ws = torch.empty(X.decode_workspace_size(probe, batch, hq, columns, True), dtype=torch.uint8,
                      device="cuda")
     eager_cache, eager_w = fresh()
     graphs = []
