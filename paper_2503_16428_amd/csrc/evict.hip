@@ -7,7 +7,8 @@
 //   evict_collect  sums the row's histograms, finds the digit of the last place,
 //                  lists the chunk's tokens that have it and counts their next
 //                  11 bits;
-//   evict_emit     finds that digit, and the last 10 bits from the row's lists;
+//   evict_emit     finds that digit, and the last 10 bits from the row's lists (if
+//                  not all of the digit's tokens are kept);
 //                  the places of a chunk's tokens follow from the counts of the
 //                  chunks before it, and it writes its kept tokens.
 // Rows of at most two chunks are one workgroup's, in one launch (evict_select).
@@ -77,7 +78,7 @@ __device__ __forceinline__ void count(int* hist, int d, bool in) {
 struct SelectShared {
   int hist[kCopies][kBins];
   int above[kSelWaves], equal[kSelWaves], sums[kSelWaves];
-  int digit, left, listed;
+  int digit, left, size, listed;
 };
 
 // Sum of the first n of the waves' numbers in LDS, in every lane.
@@ -106,7 +107,7 @@ __device__ __forceinline__ void store(const SelectShared& s, int* to) {
 }
 
 // The bin of the `take`-th largest of `parts` histograms that lie `stride` apart,
-// and the place in it that is wanted.
+// how many it has, and the place in it that is wanted.
 __device__ __forceinline__ void find(SelectShared& s, const int* hist, int parts, int stride,
                                      int take) {
   static_assert(kBins == 2 * kSelThreads, "two bins a thread");
@@ -133,8 +134,21 @@ __device__ __forceinline__ void find(SelectShared& s, const int* hist, int parts
     const bool second = take > before + n0;
     s.digit = low + !second;
     s.left = take - before - (second ? n0 : 0);
+    s.size = second ? n1 : n0;
   }
   __syncthreads();
+}
+
+// Whether all of the bin that was found are kept, whatever their other bits: the
+// rank `last` of a bin's lowest is then made one less, of which none are (`take`).
+// It is not 0: below these there are tokens that are not kept. It saves passes where
+// the upper bits tell the weights apart: 2000 tokens of 8 heads 15.2 -> 13.4 us, 4 x
+// 16,000 41.3 -> 40.6.
+__device__ __forceinline__ bool all_kept(const SelectShared& s, uint32_t& last, int& take) {
+  if (take != s.size) return false;
+  --last;
+  take = 0;
+  return true;
 }
 
 // A workgroup's place: its row's length and tokens, and its lanes' weights.
@@ -272,6 +286,7 @@ __global__ __launch_bounds__(kSelThreads) void evict_select(EvictParams p) {
       find(s, s.hist[0], kCopies, kBins, take);
       last |= (uint32_t)s.digit << shift;
       take = s.left;
+      if (all_kept(s, last, take)) break;
     }
   }
   write_kept(p, k, s, last, take, 0, 0);
@@ -356,13 +371,15 @@ __global__ __launch_bounds__(kSelThreads) void evict_emit(EvictParams p) {
         }
       }
     };
-    each_listed(chunks, [&](bool in, uint32_t r) {
-      count(s.hist[wave % kCopies], r & 1023, in && (r ^ last) >> 10 == 0);
-    });
-    __syncthreads();
-    find(s, s.hist[0], kCopies, kBins, take);
-    last |= s.digit;
-    take = s.left;
+    if (!all_kept(s, last, take)) {
+      each_listed(chunks, [&](bool in, uint32_t r) {
+        count(s.hist[wave % kCopies], r & 1023, in && (r ^ last) >> 10 == 0);
+      });
+      __syncthreads();
+      find(s, s.hist[0], kCopies, kBins, take);
+      last |= s.digit;
+      take = s.left;
+    }
     int above = 0, equal = 0;
     each_listed(k.index, [&](bool in, uint32_t r) {
       above += __popcll(__ballot(in && r > last));
@@ -454,8 +471,8 @@ hipError_t launch_evict(const CacheParams& c, bool e4m3, int batch, const int32_
                         chunks, new_pages << c.shift,        kept, new_lens, new_weights,
                         (int*)(at + s.hist), (uint32_t*)(at + s.list),
                         (ChunkCounts*)(at + s.counts), (RowDigit*)(at + s.digits)};
-  // one launch where one workgroup has the row: 2000 tokens of 8 heads 22.6 -> 15.0
-  // us, 4 x 8000 40.0 -> 30.1, 4 x 16,000 45.1 -> 41.8
+  // one launch where one workgroup has the row (before passes could be saved: 2000
+  // tokens of 8 heads 22.6 -> 15.0 us, 4 x 8000 40.0 -> 30.1, 4 x 16,000 45.1 -> 41.8)
   void (*const one[])(EvictParams) = {c.capacity() <= kChunk ? evict_select<kSteps>
                                                              : evict_select<2 * kSteps>};
   void (*const three[])(EvictParams) = {evict_count, evict_collect, evict_emit};

@@ -682,6 +682,25 @@ def test_evict_of_long_rows(kind):
     check_evict(w[:1, :, :16000].contiguous(), [15990], 64, 1, 15989, 0, False)
 
 
+@pytest.mark.parametrize("columns", [24, 300])
+@pytest.mark.parametrize("unit", [None, 2.0 ** -13, 2.0 ** -23])
+def test_evict_of_whole_groups(unit, columns):
+    """Weights in groups of seven that differ in their upper 11, 22 or 32 bits only, the last place
+    at a group's end, before and behind it; and the same with some of every group a little more."""
+    n = columns * 64 - 5
+    at = torch.randperm(columns * 64, generator=gen(76))
+    group = (at // 7).float().view(1, 1, -1)
+    w = 1 + group * unit if unit else torch.exp2(-group.clamp(max=100))
+    more = w * (1 + 2.0 ** -22 * (at % 3).float().view(1, 1, -1))
+    for x in (w, more):
+        ranked = x[0, 0, :n].sort(descending=True).values
+        ends = (torch.nonzero(ranked[1:] != ranked[:-1]).flatten() + 1).tolist()
+        for end in (ends[0], ends[40]):
+            for budget in (end - 1, end, end + 1):
+                check_evict(x, [n], 64, 1, max(budget, 1), 0, False)
+    check_evict(-w, [n], 64, 1, 777, 0, True)
+
+
 @pytest.mark.parametrize("seed", range(12))
 def test_evict_of_random_shapes(seed):
     rng = random.Random(500 + seed)
