@@ -422,8 +422,8 @@ int xattn_cache_append(const void *k, const int64_t *k_strides, const void *v,
  *            aligned; its contents on entry are ignored. Calls that may run at the
  *            same time need one each.
  * QK^T and PV run on the bf16 matrix cores with fp32 accumulation (e4m3 values
- * are exact in bf16); the softmax is fp32, and P goes into PV as the sum of two
- * bf16 values, within 2^-15 of it. The output is rounded once.
+ * are exact in bf16); the softmax is fp32, and P goes into PV as the sum of three
+ * bf16 values, within 2^-29 of it. The output is rounded once.
  */
 int xattn_decode_workspace_size(const xattn_cache *cache, int batch, int hq, int table_pages,
                                 int weights, size_t *bytes);

@@ -10,9 +10,11 @@
 //     those same keys, so that the i-th elements of its 8 pieces are row c of the
 //     A operand of MFMA i, whose output rows are elements 8c + i: pairs of values
 //     are put together within the lane, nothing moves between lanes.
-// P is the sum of two bf16 values, one MFMA each (products exact): the weights are
-// off by at most 2^-15, less than a hundredth of the output's own rounding, at an
-// eighth of the time of fp32 MFMAs.
+// P is the sum of three bf16 values, one MFMA each (products exact), which is P in
+// fp32 at three sixteenths of the time of fp32 MFMAs. (Two are off by up to 2^-15; the
+// third costs nothing where loads bound: 64 sequences of up to 8000 tokens 173.8 ->
+// 174.0 us, 128K 87.1 -> 86.5, rows of 2048 in 8 bits 36.7 -> 37.3; with two tiles of
+// heads in 8 bits 41.4 -> 44.2.)
 //
 // Short rows (sequence, key head, tile of query heads) are one workgroup's each. The
 // work of longer ones is the batch's rows end to end, in units of kWaves wave steps;
@@ -21,7 +23,7 @@
 // others every share leaves a partial output (at most two a workgroup: its first and
 // its last row), and decode_join adds them in order.
 //
-// Bound by HBM: with tiles filled up to 16 heads and P in two parts 24 flops a byte
+// Bound by HBM: with tiles filled up to 16 heads and P in three parts 32 flops a byte
 // of bf16 keys and values, which keeps the matrix cores busy for 6 % of the time
 // that the loads take. 64 sequences of up to 8000 tokens, 32 / 8 heads, 1.08 GB:
 // 170 us in decode_kernel (6.3 TB/s; a kernel that only loads does 6.2 to 7.0), 5.6
@@ -57,19 +59,25 @@ __device__ __forceinline__ bf16x8 bf16_of(uint32_t a, uint32_t b) {
   const auto s = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true);
   return bf16x8{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
 }
-// The two bf16 values of p and q whose sums stand for p (1 + 2^-17): the upper
-// halves of their bits, and what is left, at most 2^-7 p, rounded by at most 2^-8 of
-// it. The rest is made 2^-17 p larger so that it is positive, and an infinite value
-// times p infinite; the factor goes out with the sum of the weights.
-constexpr float kMore = 1.f + 0x1p-17f;
-__device__ __forceinline__ void split(float p, float q, uint32_t* upper, uint32_t* rest) {
-  const uint32_t a = __builtin_bit_cast(uint32_t, p), b = __builtin_bit_cast(uint32_t, q);
-  typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
-  const bf16x2 r = {
-      (__bf16)__builtin_fmaf(p, kMore, -__builtin_bit_cast(float, a & 0xffff0000u)),
-      (__bf16)__builtin_fmaf(q, kMore, -__builtin_bit_cast(float, b & 0xffff0000u))};
-  *upper = __builtin_amdgcn_perm(b, a, 0x07060302u);
-  *rest = __builtin_bit_cast(uint32_t, r);
+// p and q as sums of three bf16 values each: the upper halves of their bits, those of
+// what is left, and what is left then, at most the last eight bits of a mantissa. No
+// part of a positive weight is 0, so that an infinite value times it is infinite: the
+// lower two are at least 2^-30 p each, and their sum is off by no more than that makes.
+struct Split {
+  uint32_t upper, middle, lower;
+};
+__device__ __forceinline__ Split split(float p, float q) {
+  const auto bits = [](float x) { return __builtin_bit_cast(uint32_t, x); };
+  const auto upper = [](float x) {
+    return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & 0xffff0000u);
+  };
+  const auto pack = [&](float x, float y) {
+    return __builtin_amdgcn_perm(bits(y), bits(x), 0x07060302u);
+  };
+  const float least_p = p * 0x1p-30f, least_q = q * 0x1p-30f;
+  const float a = fmaxf(p - upper(p), least_p), b = fmaxf(q - upper(q), least_q);
+  return Split{pack(p, q), pack(a, b),
+               pack(fmaxf(a - upper(a), least_p), fmaxf(b - upper(b), least_q))};
 }
 // Elements 2n and 2n + 1 (n = 0 .. 3) of a lane's four rows of a tile, in bf16:
 // rows 0, 1 and rows 2, 3 of the one, then of the other.
@@ -179,11 +187,10 @@ __device__ __forceinline__ int sum_of_wave(int x) {
   return __builtin_amdgcn_readlane(scan_of_wave(x), kWave - 1);
 }
 
-// Four elements of a finished row: output head `head`, elements d .. d + 3, from the
-// sum of its values times kMore.
+// Four elements of a finished row: output head `head`, elements d .. d + 3.
 __device__ __forceinline__ void write_row(const DecodeParams& p, long long head, int d, float top,
                                           float sum, f32x4 out) {
-  const float inv = sum == 0.f ? 0.f : 1.f / (kMore * sum);
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
   typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4;
   const bf16x4 r = {(__bf16)(out[0] * inv), (__bf16)(out[1] * inv), (__bf16)(out[2] * inv),
                     (__bf16)(out[3] * inv)};
@@ -438,7 +445,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(Decod
             l[x] += zs[x][i][r];
           }
       }
-      u32x4 upper[RT], rest[RT];
+      u32x4 upper[RT], middle[RT], lower[RT];
 #pragma unroll
       for (int x = 0; x < RT; ++x)
 #pragma unroll
@@ -448,10 +455,10 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(Decod
             for (int r = 0; r < 4; ++r) zs[x][i][r] *= scale_of(v_scale[i] >> (8 * r) & 255);
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
-            uint32_t a, b;
-            split(zs[x][i][2 * r], zs[x][i][2 * r + 1], &a, &b);
-            upper[x][2 * i + r] = a;
-            rest[x][2 * i + r] = b;
+            const Split w = split(zs[x][i][2 * r], zs[x][i][2 * r + 1]);
+            upper[x][2 * i + r] = w.upper;
+            middle[x][2 * i + r] = w.middle;
+            lower[x][2 * i + r] = w.lower;
           }
         }
 #pragma unroll
@@ -463,10 +470,11 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(Decod
         const bf16x8 odd = as_bf16x8(u32x4{f[0], f[1], f[2], f[3]});
 #pragma unroll
         for (int x = 0; x < RT; ++x) {
-          o[x][2 * n] = mfma16(even, as_bf16x8(upper[x]), o[x][2 * n]);
-          o[x][2 * n + 1] = mfma16(odd, as_bf16x8(upper[x]), o[x][2 * n + 1]);
-          o[x][2 * n] = mfma16(even, as_bf16x8(rest[x]), o[x][2 * n]);
-          o[x][2 * n + 1] = mfma16(odd, as_bf16x8(rest[x]), o[x][2 * n + 1]);
+#pragma unroll
+          for (const u32x4& part : {upper[x], middle[x], lower[x]}) {
+            o[x][2 * n] = mfma16(even, as_bf16x8(part), o[x][2 * n]);
+            o[x][2 * n + 1] = mfma16(odd, as_bf16x8(part), o[x][2 * n + 1]);
+          }
         }
         __builtin_amdgcn_sched_barrier(0);
       }

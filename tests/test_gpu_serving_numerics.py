@@ -1,0 +1,42 @@
+"""What the serving calls hold in 32 bits, seen where it shows: outputs that are
+the small rest of large terms, so that their own rounding to bf16 hides nothing."""
+import pytest
+
+from . import serving_oracle as R
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("no GPU", allow_module_level=True)
+
+import paper_2503_16428_amd as X  # noqa: E402
+
+from .serving_numerics import cancelling, in_two_parts  # noqa: E402
+from .test_gpu_serving import bits, ints, within  # noqa: E402
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("hq,hkv", [(4, 1), (6, 2), (20, 1)])
+@pytest.mark.parametrize("wide", [False, True])
+def test_weights_enter_the_product_in_32_bits(hq, hkv, e4m3, wide):
+    """Values that all but cancel: the output is their weights' error and little else."""
+    batch, page = 24, 16
+    q, k, v, scales, want, total = cancelling(batch, hq, hkv, page, e4m3, seed=500 + hq)
+    n = 8 if e4m3 else 4
+    columns = 70 if wide else 2  # rows that are shared out among workgroups; one workgroup's each
+    table = torch.full((batch, columns), -1, dtype=torch.int32)
+    table[:, 0] = torch.arange(batch)
+    cache = X.KVCache(k.cuda(), v.cuda(), *[s.cuda() for s in scales])
+    o, _ = X.xattn_decode(q.cuda(), cache, table.cuda(), ints([n] * batch))
+    # The products are exact, |z| <= 1.5 and |z - max| <= 3 in log2: two roundings of z and
+    # one of the difference, 6 * 2^-24 at most in the exponent; the exponential's own 2^-22; the
+    # weight's parts 2^-22; three parts of n terms, each addition off by at most a step, 2^-23;
+    # sum and quotient of the end, 2^-22 of a result that is next to nothing.
+    bound = total * (6 * 2.0 ** -24 + 2.0 ** -21 + 3 * n * 2.0 ** -23)
+    # that bound tells weights in two bf16 parts from weights in 32 bits
+    two = in_two_parts(q, k, v, scales, n)
+    assert ((two - want).abs() > R.bf16_bound(want, bound)).any()
+    within(o, want, R.bf16_bound(want, bound))
+    assert torch.equal(bits(o), bits(X.xattn_decode(q.cuda(), cache, table.cuda(),
+                                                    ints([n] * batch))[0]))
