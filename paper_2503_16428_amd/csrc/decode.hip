@@ -135,16 +135,6 @@ struct PieceOf<true> {
   typedef u32x2 type;
 };
 
-// Workgroups that share a batch's units: two a CU, or three, as many as are
-// resident, where rows are many and a workgroup often begins a new one, which the
-// others of its CU then make up for. In us, two / three a CU, 8 key heads: one
-// sequence of 128K 88 / 92, 4 of 32K 88 / 91, 48 of up to 8000 133 / 138, in 8 bits
-// 72 / 78; 64 of up to 8000 183 / 177, 100 / 95, of up to 2000 63 / 59, 44 / 39;
-// 64 of 2048, a row each, 88 / 96. (Any number that is no multiple of the CUs
-// gives some of them more work: 384, 103 us at 128K.)
-constexpr int kMostWorkers = 768;
-inline int most_workers(int rows) { return rows >= 512 ? kMostWorkers : 512; }
-
 // How `units` are shared out: the first `more` workgroups have per + 1 of them,
 // the others per; no more workgroups than half the units (one key head, 64K: 20.4
 // -> 16.8 us for the fewer parts to join).
@@ -793,7 +783,7 @@ hipError_t launch_decode(const void* q, const CacheParams& c, bool e4m3, int bat
   const bool whole = whole_rows(c, e4m3, rows);
   // no more workgroups than there can be shares
   const long long units = (long long)rows * ((c.capacity() + kUnit - 1) / kUnit);
-  p.most_workers = whole ? 0 : most_workers(rows);
+  p.most_workers = whole ? 0 : decode_workers(rows, p.tile_rows > kRows);
   if ((units + 1) / 2 < p.most_workers) p.most_workers = (int)((units + 1) / 2);
   void (*const kernels[2][2][2])(DecodeParams) = {
       {{decode_kernel<false, 1, false>, decode_kernel<false, 1, true>},

@@ -47,6 +47,21 @@ struct CacheParams {
   __host__ __device__ int capacity() const { return table_pages << shift; }
 };
 
+// Workgroups that share a decode's work: two a CU, or three where rows are many and a
+// workgroup often begins a new one, which the others of its CU then make up for. All
+// of them have to be resident, or the equal shares take a second turn: of the kernel
+// for two tiles of heads (groups of more than 16) a CU holds two. In us, two / three a
+// CU, 8 key heads, groups of 4: one sequence of 128K 88 / 92, 4 of 32K 88 / 91, 48 of
+// up to 8000 133 / 138, in 8 bits 72 / 78; 64 of up to 8000 183 / 177, 100 / 95, of up
+// to 2000 63 / 59, 44 / 39; 64 of 2048, a row each, 88 / 96. Two tiles: 512 sequences
+// of up to 4000, 32 / 1 heads, 131 / 144, in 8 bits 94 / 108, all of 4000 184 / 214;
+// 1024 of up to 2000 168 / 190; 600 of up to 2500, 20 / 1 heads, 101 / 115. (Any number
+// that is no multiple of the CUs gives some of them more work: 384, 103 us at 128K.)
+constexpr int kMostWorkers = 768;
+inline int decode_workers(int rows, bool two_tiles) {
+  return rows >= 512 && !two_tiles ? kMostWorkers : 512;
+}
+
 }  // namespace xattn
 
 hipError_t launch_rotary(const void* x, const xattn::Strides& xs, int batch, int heads, int tokens,

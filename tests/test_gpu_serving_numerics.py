@@ -13,7 +13,7 @@ if not torch.cuda.is_available():
 import paper_2503_16428_amd as X  # noqa: E402
 
 from .serving_numerics import cancelling, in_two_parts  # noqa: E402
-from .test_gpu_serving import bits, ints, within  # noqa: E402
+from .test_gpu_serving import bits, check_decode, decode_case, ints, within  # noqa: E402
 
 
 @pytest.mark.parametrize("e4m3", [False, True])
@@ -40,3 +40,10 @@ def test_weights_enter_the_product_in_32_bits(hq, hkv, e4m3, wide):
     within(o, want, R.bf16_bound(want, bound))
     assert torch.equal(bits(o), bits(X.xattn_decode(q.cuda(), cache, table.cuda(),
                                                     ints([n] * batch))[0]))
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_decode_of_many_rows_of_wide_groups(e4m3):
+    """More than 512 rows of two tiles of heads: 512 workgroups share them."""
+    lens = [(11 * i) % 23 for i in range(520)]
+    check_decode(*decode_case(520, 17, 1, 16, lens, e4m3, spare=0, columns=66), lens)
