@@ -58,3 +58,33 @@ def in_two_parts(q, k, v, scales, n):
     parts = upper.double() + rest.double()
     per_head = v[:, :, :n].double().repeat_interleave(q.shape[1] // k.shape[1], 1)
     return (parts.unsqueeze(-1) * per_head).sum(2) / (more * p.double().sum(-1, keepdim=True))
+
+
+def rotated_in_8_bits(k, pos, pairs, freq, interleaved):
+    """(least, most, bytes): the e4m3 values that keys k [batch, heads, tokens, 128], rotated and
+    scaled, may round to if their angles are good to 2^-50 of themselves and their sines to
+    1e-12, and the scales' bytes. Nearly everywhere least and most are the same."""
+    out, _ = R.rotate(k, pos, pairs, freq, interleaved)
+    off = torch.zeros_like(out)
+    axis = [a for a, n in enumerate(pairs) for _ in range(n)]
+    for i, f in enumerate(freq):
+        m, n = (2 * i, 2 * i + 1) if interleaved else (i, i + 64)
+        phi = (pos[axis[i]].double() * f).abs().unsqueeze(1)
+        both = k[..., m].double().abs() + k[..., n].double().abs()
+        off[..., m] = off[..., n] = both * (phi * 2.0 ** -50 + 1e-12)
+    least, scale, _ = R.e4m3(out - off, k, interleaved)
+    most, _, _ = R.e4m3(out + off, k, interleaved)
+    return least, most, scale
+
+
+def rotated_in_fp32(k, pos, pairs, freq, interleaved):
+    """The same values if the keys are turned in 32 bits: the turn in 64, all behind it not."""
+    out = k.float().clone()
+    axis = [a for a, n in enumerate(pairs) for _ in range(n)]
+    for i, f in enumerate(freq):
+        m, n = (2 * i, 2 * i + 1) if interleaved else (i, i + 64)
+        turn = pos[axis[i]].double() * (f / (2 * math.pi))
+        phi = ((turn - turn.round()).float() * (2 * math.pi)).unsqueeze(1)
+        a, b = k[..., m].float(), k[..., n].float()
+        out[..., m], out[..., n] = a * phi.cos() - b * phi.sin(), a * phi.sin() + b * phi.cos()
+    return R.e4m3(out, k, interleaved)[0]

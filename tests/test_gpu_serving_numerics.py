@@ -12,7 +12,8 @@ if not torch.cuda.is_available():
 
 import paper_2503_16428_amd as X  # noqa: E402
 
-from .serving_numerics import cancelling, in_two_parts  # noqa: E402
+from .serving_numerics import (cancelling, in_two_parts, rotated_in_8_bits,  # noqa: E402
+                               rotated_in_fp32)
 from .test_gpu_serving import bits, check_decode, decode_case, ints, within  # noqa: E402
 
 
@@ -47,3 +48,27 @@ def test_decode_of_many_rows_of_wide_groups(e4m3):
     """More than 512 rows of two tiles of heads: 512 workgroups share them."""
     lens = [(11 * i) % 23 for i in range(520)]
     check_decode(*decode_case(520, 17, 1, 16, lens, e4m3, spare=0, columns=66), lens)
+
+
+@pytest.mark.parametrize("pairs,interleaved", [([64], False), ([16, 24, 24], True), ([20, 30], False)])
+def test_keys_that_go_to_8_bits_are_turned_in_64(pairs, interleaved):
+    """Every byte, of enough keys that turning them in 32 bits gives other ones."""
+    hkv, tokens, page = 4, 6000, 64
+    g = torch.Generator().manual_seed(540)
+    k = (torch.randn((1, hkv, tokens, 128), generator=g) * 2.5).bfloat16()
+    pos = torch.randint(0, 100000, (len(pairs), 1, tokens), generator=g, dtype=torch.int32)
+    freq = R.freqs(pairs)
+    least, most, scale = rotated_in_8_bits(k, pos, pairs, freq, interleaved)
+    assert (bits(least) != bits(most)).double().mean() < 1e-6
+    other = bits(rotated_in_fp32(k, pos, pairs, freq, interleaved))
+    assert ((other != bits(least)) & (other != bits(most))).any()
+    pages = -(-tokens // page)
+    cache = X.KVCache.empty(pages, hkv, page, torch.float8_e4m3fn)
+    table = torch.randperm(pages, generator=g).int().view(1, pages)
+    X.xattn_cache_append(k.cuda(), k.cuda(), cache, table.cuda(), ints([0]), pos=pos.cuda(),
+                         rotary=X.Rotary(pairs, freq, interleaved))
+    order = table[0].long()
+    got = bits(cache.k)[order].transpose(0, 1).reshape(hkv, -1, 128)[:, :tokens]
+    byte = cache.k_scale.cpu()[order].transpose(0, 1).reshape(hkv, -1)[:, :tokens]
+    assert torch.equal(byte, scale[0])
+    assert ((got == bits(least)[0]) | (got == bits(most)[0])).all()
