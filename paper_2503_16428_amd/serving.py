@@ -40,10 +40,27 @@ def rotary_freqs(pairs, base: float = 10000.0, restart: bool = False) -> np.ndar
     return float(base) ** (-np.arange(n) / n)
 
 
-class Rotary:
+class _Fixed:
+    """An object whose C struct holds what its attributes of _FIXED say: neither changes once it
+    is made."""
+    _FIXED = frozenset()
+
+    def __setattr__(self, name, value):
+        if name in self._FIXED and "_ref" in self.__dict__:  # the last that is set
+            _fail(f"the {name} of a {type(self).__name__} is fixed: make another one")
+        super().__setattr__(name, value)
+
+    def __delattr__(self, name):
+        if name in self._FIXED:
+            _fail(f"the {name} of a {type(self).__name__} is fixed")
+        super().__delattr__(name)
+
+
+class Rotary(_Fixed):
     """Rotary positions of one model: pairs[a] of a head's 64 pairs turn with position axis a, by
     freq (float64, one a pair, radians per position); pair i is elements (2i, 2i+1) if interleaved,
     else (i, i+64). Pairs behind them are not rotated."""
+    _FIXED = frozenset(("axes", "pairs", "interleaved", "_freq", "_plan", "_ref"))
 
     def __init__(self, pairs, freq, interleaved: bool = False):
         pairs = [int(n) for n in pairs]
@@ -59,9 +76,12 @@ class Rotary:
         self._ref = ctypes.byref(self._plan)
 
 
-class KVCache:
+class KVCache(_Fixed):
     """A pool of pages: k, v [pages, hkv, page, 128], bf16, or float8_e4m3fn with the bytes of
-    their power-of-two scales k_scale, v_scale uint8 [pages, hkv, page]."""
+    their power-of-two scales k_scale, v_scale uint8 [pages, hkv, page]. A larger pool is another
+    KVCache."""
+    _FIXED = frozenset(("k", "v", "k_scale", "v_scale", "pages", "hkv", "page", "e4m3", "device",
+                        "_struct", "_ref"))
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
         if k.dim() != 4 or k.shape[3] != HEAD_DIM or k.shape[2] not in _PAGES or 0 in k.shape:
