@@ -142,9 +142,26 @@ def _here(first, others, names, dense=()):
 
 
 def _is(t, shape, dtype, name):
-    """_check_shape, at the cost of two comparisons where all is well."""
-    if t is not None and (t.shape != shape or t.dtype is not dtype):
+    """_check_shape of a tensor that must be given, at the cost of two comparisons where all is
+    well."""
+    if t is None:
+        _fail(f"{name} must be given")
+    if t.shape != shape or t.dtype is not dtype:
         _check_shape(t, shape, dtype, name)
+
+
+def _may_be(t, shape, dtype, name):
+    """The same of one that may be None."""
+    if t is not None:
+        _is(t, shape, dtype, name)
+
+
+def _int32(value, name):
+    """A number that goes to C as 32 bits, where a larger one would become another."""
+    n = int(value)
+    if not -2**31 <= n < 2**31:
+        _fail(f"{name} must fit 32 bits, got {n}")
+    return n
 
 
 @functools.lru_cache(maxsize=1024)
@@ -250,7 +267,7 @@ def xattn_cache_append(k, v, cache: KVCache, table, start, count=None, pos=None,
         _fail(f"k has {h} heads, the cache {cache.hkv}")
     width = _table(table, b)
     _is(start, (b,), torch.int32, "start")
-    _is(count, (b,), torch.int32, "count")
+    _may_be(count, (b,), torch.int32, "count")
     if (pos is None) != (rotary is None):
         _fail("pos and rotary go together")
     if rotary is not None:
@@ -277,8 +294,8 @@ def decode_workspace_size(cache: KVCache, batch: int, hq: int, table_pages: int,
                           weights: bool = False) -> int:
     """Bytes of xattn_decode's workspace."""
     _is_cache(cache)
-    return _decode_bytes(cache.hkv, cache.page, cache.e4m3, int(batch), int(hq), int(table_pages),
-                         int(bool(weights)))
+    return _decode_bytes(cache.hkv, cache.page, cache.e4m3, _int32(batch, "batch"),
+                         _int32(hq, "hq"), _int32(table_pages, "table_pages"), int(bool(weights)))
 
 
 def xattn_decode(q, cache: KVCache, table, lens, o=None, lse=None, weights=None, workspace=None,
@@ -295,9 +312,9 @@ def xattn_decode(q, cache: KVCache, table, lens, o=None, lse=None, weights=None,
     b, hq, _ = shape
     width = _table(table, b)
     _is(lens, (b,), torch.int32, "lens")
-    _is(o, shape, torch.bfloat16, "o")
-    _is(lse, (b, hq), torch.float32, "lse")
-    _is(weights, (b, cache.hkv, width * cache.page), torch.float32, "weights")
+    _may_be(o, shape, torch.bfloat16, "o")
+    _may_be(lse, (b, hq), torch.float32, "lse")
+    _may_be(weights, (b, cache.hkv, width * cache.page), torch.float32, "weights")
     _check_workspace(workspace)
     dense = (q, table, lens, o, lse, weights, workspace)
     at = _here(q, (table, lens, cache.k, o, lse, weights, workspace),
@@ -329,7 +346,8 @@ def _evict_bytes(hkv, page, batch, table_pages):
 def evict_workspace_size(cache: KVCache, batch: int, table_pages: int) -> int:
     """Bytes of xattn_cache_evict's workspace."""
     _is_cache(cache)
-    return _evict_bytes(cache.hkv, cache.page, int(batch), int(table_pages))
+    return _evict_bytes(cache.hkv, cache.page, _int32(batch, "batch"),
+                        _int32(table_pages, "table_pages"))
 
 
 def xattn_cache_evict(cache: KVCache, table, lens, weights, new_table, budget: int, recent: int,
@@ -342,16 +360,18 @@ def xattn_cache_evict(cache: KVCache, table, lens, weights, new_table, budget: i
     _is_cache(cache)
     if table.dim() != 2:
         _fail(f"table must be [batch, pages], got {tuple(table.shape)}")
-    b, h, budget = table.shape[0], cache.hkv, int(budget)
+    b, h, budget, recent = table.shape[0], cache.hkv, int(budget), int(recent)
     width, new_width = _table(table, b), _table(new_table, b, "new_table")
     _is(lens, (b,), torch.int32, "lens")
     _is(weights, (b, h, width * cache.page), torch.float32, "weights")
     if not 1 <= budget <= new_width * cache.page:
         _fail(f"budget must be 1 to {new_width * cache.page} (the new table's tokens), got "
               f"{budget}")
-    _is(kept, (b, h, budget), torch.int32, "kept")
-    _is(new_lens, (b,), torch.int32, "new_lens")
-    _is(new_weights, (b, h, new_width * cache.page), torch.float32, "new_weights")
+    if not 0 <= recent <= budget:
+        _fail(f"recent must be 0 to {budget} (the budget), got {recent}")
+    _may_be(kept, (b, h, budget), torch.int32, "kept")
+    _may_be(new_lens, (b,), torch.int32, "new_lens")
+    _may_be(new_weights, (b, h, new_width * cache.page), torch.float32, "new_weights")
     _check_workspace(workspace)
     tensors = (lens, weights, new_table, kept, new_lens, new_weights, workspace)
     at = _here(table, (*tensors, cache.k), ("table", "lens", "weights", "new_table", "kept",
@@ -370,7 +390,7 @@ def xattn_cache_evict(cache: KVCache, table, lens, weights, new_table, budget: i
 
     kept, new_lens, new_weights, workspace = _made(stream, allocate)
     _check(lib().xattn_cache_evict(cache._ref, b, _ptr(table), width, _ptr(lens), _ptr(weights),
-                                   budget, int(recent), _ptr(new_table), new_width, _ptr(kept),
+                                   budget, recent, _ptr(new_table), new_width, _ptr(kept),
                                    _ptr(new_lens), _ptr(new_weights), _ptr(workspace),
                                    0 if workspace is None else workspace.numel(),
                                    _handle(stream, at)))
