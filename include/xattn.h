@@ -323,6 +323,10 @@ int xattn_head_error_mean(const void *o, const void *o_ref, const xattn_dims *di
  * array of bfloat16 or cache values is 16-byte aligned. Read during the call only.
  */
 
+/* What a call writes (outputs, weights, workspace; in xattn_cache_append the places
+ * of the new tokens) shares no memory with what it reads or with anything else it
+ * writes, but where a call says so; XATTN_ERR_ARG where the host can see that it does. */
+
 /* Rotary positions: the 64 pairs of a head are shared out among `axes` position
  * axes (e.g. time, height, width), pairs[a] to axis a in order; the pairs
  * behind them are not rotated.
@@ -411,7 +415,7 @@ int xattn_cache_append(const void *k, const int64_t *k_strides, const void *v,
  * page holds behind the last token has no effect, whatever it is.
  * Several new tokens of one sequence are several rows with the same pages and
  * each its own length.
- *   q        bf16 [batch][hq][128]; o the same (output)
+ *   q        bf16 [batch][hq][128]; o the same (output; may be q itself)
  *   lens     int32 [batch] device
  *   lse      fp32 [batch][hq] (output) or NULL
  *   weights  fp32 [batch][hkv][table_pages * page], 16-byte aligned (updated), or
@@ -447,9 +451,9 @@ int xattn_decode(const void *q, const xattn_cache *cache, int batch, int hq,
  *                `table`; new_pages * page >= budget
  *   kept         int32 [batch][hkv][budget] (output): the tokens kept, ascending,
  *                -1 behind them
- *   new_lens     int32 [batch] (output): min(lens, budget); must not be lens
+ *   new_lens     int32 [batch] (output): min(lens, budget)
  *   new_weights  fp32 [batch][hkv][new_pages * page] (output): the kept tokens'
- *                weights, 0 behind them; no memory of weights
+ *                weights, 0 behind them
  *   workspace    as for xattn_decode, xattn_evict_workspace_size() bytes (0 for
  *                rows of up to 16384 tokens, then it may be NULL)
  * The weights are 16-byte aligned. 1 <= budget, 0 <= recent <= budget. Page rows

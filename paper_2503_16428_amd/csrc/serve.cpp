@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "serve.h"
 #include "xattn.h"
@@ -157,6 +158,24 @@ int check_workspace(const void* workspace, size_t bytes, size_t need) {
   return XATTN_OK;
 }
 
+// Arrays that are to lie apart, as far as one of two is written: bytes [at, at + bytes).
+struct Extent {
+  const char* name;
+  const void* at;  // NULL: not given
+  size_t bytes;
+  bool written;
+};
+int check_apart(std::initializer_list<Extent> all) {
+  for (auto a = all.begin(); a != all.end(); ++a)
+    for (auto b = all.begin(); b != a; ++b) {
+      if (!a->at || !b->at || !(a->written || b->written)) continue;
+      const uintptr_t x = (uintptr_t)a->at, y = (uintptr_t)b->at;
+      if (x < y + b->bytes && y < x + a->bytes)
+        return fail(XATTN_ERR_ARG, "%s and %s share memory", b->name, a->name);
+    }
+  return XATTN_OK;
+}
+
 int check_decode(const xattn_cache* cache, int batch, int hq, const int32_t* table,
                  int table_pages, CacheParams* c) {
   int rc;
@@ -173,6 +192,12 @@ int check_decode(const xattn_cache* cache, int batch, int hq, const int32_t* tab
     return fail(XATTN_ERR_UNSUPPORTED, "more than 2^30 units of 128 keys and 32 heads a batch");
   return XATTN_OK;
 }
+
+// Bytes of a cache's keys (or values), and of their scales.
+size_t vector_bytes(const CacheParams& c, bool e4m3) {
+  return ((size_t)c.pages * c.hkv << c.shift) * xattn::kHeadDim * (e4m3 ? 1 : 2);
+}
+size_t scale_bytes(const CacheParams& c) { return (size_t)c.pages * c.hkv << c.shift; }
 
 int check_evict(const xattn_cache* cache, const int32_t* table, int table_pages, int batch,
                 CacheParams* c) {
@@ -258,6 +283,21 @@ int xattn_decode(const void* q, const xattn_cache* cache, int batch, int hq,
   const bool e4m3 = cache->type == XATTN_CACHE_E4M3;
   const size_t need = decode_scratch_bytes(c, e4m3, batch, hq, weights != nullptr);
   if ((rc = check_workspace(workspace, workspace_bytes, need))) return rc;
+  const size_t rows = (size_t)batch * hq, vectors = vector_bytes(c, e4m3);
+  const size_t q_bytes = rows * xattn::kHeadDim * 2;
+  if ((rc = check_apart(
+           {{"q", o == q ? nullptr : q, q_bytes, false},  // a head's q is read before its o is written
+            {"table", table, (size_t)batch * table_pages * 4, false},
+            {"lens", lens, (size_t)batch * 4, false},
+            {"the cache's k", c.k, vectors, false},
+            {"the cache's v", c.v, vectors, false},
+            {"the cache's k_scale", c.k_scale, scale_bytes(c), false},
+            {"the cache's v_scale", c.v_scale, scale_bytes(c), false},
+            {"o", o, q_bytes, true},
+            {"lse", lse, rows * 4, true},
+            {"weights", weights, (size_t)batch * c.hkv * c.capacity() * 4, true},
+            {"workspace", need ? workspace : nullptr, need, true}})))
+    return rc;
   return launched(launch_decode(q, c, e4m3, batch, hq, lens, o, lse, weights, workspace,
                                 (hipStream_t)stream),
                   "xattn_decode");
@@ -294,11 +334,26 @@ int xattn_cache_evict(const xattn_cache* cache, int batch, const int32_t* table,
       (rc = check_pointer(new_lens, "new_lens", 4)) ||
       (rc = check_pointer(new_weights, "new_weights", 4)))
     return rc;
-  if (new_lens == lens || new_weights == weights || new_table == table)
-    return fail(XATTN_ERR_ARG, "an output is its own input, or new_table is table");
+  if (new_table == table) return fail(XATTN_ERR_ARG, "new_table is table");
+  const size_t rows = (size_t)batch * c.hkv;
   const size_t need = evict_scratch_bytes(c, batch);
+  const bool e4m3 = cache->type == XATTN_CACHE_E4M3;
   if ((rc = check_workspace(workspace, workspace_bytes, need))) return rc;
-  return launched(launch_evict(c, cache->type == XATTN_CACHE_E4M3, batch, lens, weights, budget,
+  if ((rc = check_apart(
+           {{"table", table, (size_t)batch * table_pages * 4, false},
+            {"lens", lens, (size_t)batch * 4, false},
+            {"weights", weights, rows * c.capacity() * 4, false},
+            {"new_table", new_table, (size_t)batch * new_pages * 4, false},
+            {"the cache's k", c.k, vector_bytes(c, e4m3), false},
+            {"the cache's v", c.v, vector_bytes(c, e4m3), false},
+            {"the cache's k_scale", c.k_scale, scale_bytes(c), false},
+            {"the cache's v_scale", c.v_scale, scale_bytes(c), false},
+            {"kept", kept, rows * budget * 4, true},
+            {"new_lens", new_lens, (size_t)batch * 4, true},
+            {"new_weights", new_weights, (rows * new_pages << c.shift) * 4, true},
+            {"workspace", need ? workspace : nullptr, need, true}})))
+    return rc;
+  return launched(launch_evict(c, e4m3, batch, lens, weights, budget,
                                recent, new_table, new_pages, kept, new_lens, new_weights,
                                workspace, (hipStream_t)stream),
                   "xattn_cache_evict");

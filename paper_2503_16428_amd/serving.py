@@ -301,7 +301,7 @@ def decode_workspace_size(cache: KVCache, batch: int, hq: int, table_pages: int,
 def xattn_decode(q, cache: KVCache, table, lens, o=None, lse=None, weights=None, workspace=None,
                  want_lse=False, stream=None):
     """Attention of one new token per sequence, q bf16 [batch, hq, 128], over its lens[b] cached
-    tokens: (o like q, lse fp32 [batch, hq] or None). weights (fp32 [batch, hkv,
+    tokens: (o like q, and may be q; lse fp32 [batch, hq] or None). weights (fp32 [batch, hkv,
     table_pages * page]), if given, grow by each key's softmax weights, summed over its heads."""
     _is_cache(cache)
     shape = q.shape
@@ -377,9 +377,6 @@ def xattn_cache_evict(cache: KVCache, table, lens, weights, new_table, budget: i
     at = _here(table, (*tensors, cache.k), ("table", "lens", "weights", "new_table", "kept",
                                             "new_lens", "new_weights", "workspace", "cache"),
                (table, *tensors))
-    for n, out, given in (("new_lens", new_lens, lens), ("new_weights", new_weights, weights)):
-        if out is not None and not _apart(out, given):
-            _fail(f"{n} must lie apart from the call's input")
     def allocate():
         need = 0 if workspace is not None else _evict_bytes(h, cache.page, b, width)
         return (lens.new_empty((b, h, budget)) if kept is None else kept,

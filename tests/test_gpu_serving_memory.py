@@ -1,0 +1,48 @@
+"""Where the serving calls may write: in place, beside their inputs in one buffer."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("no GPU", allow_module_level=True)
+
+import paper_2503_16428_amd as X  # noqa: E402
+
+from .test_gpu_serving import bits, decode_case, ints, on_gpu  # noqa: E402
+
+
+@pytest.mark.parametrize("hq,hkv,columns", [(4, 2, 4), (4, 2, 80), (40, 1, 4), (40, 1, 80)])
+def test_decode_in_place(hq, hkv, columns):
+    """o is q: whole rows and shared ones, one tile of heads and two, a row without keys."""
+    lens = [60, 0, 1, 33]
+    if columns > 4:
+        lens[0] = 1200
+    q, k, v, s, table = decode_case(4, hq, hkv, 16, lens, False, columns=columns)
+    cache, td, ld = on_gpu(k, v, s), table.cuda(), ints(lens)
+    want, lse = X.xattn_decode(q.cuda(), cache, td, ld, want_lse=True)
+    x = q.cuda()
+    o, lse2 = X.xattn_decode(x, cache, td, ld, o=x, want_lse=True)
+    assert o is x and torch.equal(bits(x), bits(want)) and torch.equal(bits(lse), bits(lse2))
+
+
+def test_outputs_may_lie_side_by_side():
+    """Outputs and workspace cut from one buffer, one behind the other."""
+    lens = [700, 1300]
+    q, k, v, s, table = decode_case(2, 4, 2, 16, lens, False, columns=90)
+    cache, qd, td, ld = on_gpu(k, v, s), q.cuda(), table.cuda(), ints(lens)
+    n = X.decode_workspace_size(cache, 2, 4, 90, True)
+    w0 = torch.rand((2, 2, 1440), device="cuda")
+    w = w0.clone()
+    want = (*X.xattn_decode(qd, cache, td, ld, weights=w, want_lse=True), w)
+    parts = [2 * 4 * 128 * 2, 2 * 4 * 4, 2 * 2 * 1440 * 4, n]
+    buffer = torch.zeros(sum(parts) + 64, dtype=torch.uint8, device="cuda")
+    at = [sum(parts[:i]) for i in range(4)]
+    o, lse, w2, ws = (buffer[a:a + m] for a, m in zip(at, parts))
+    o, lse = o.view(torch.bfloat16).view(2, 4, 128), lse.view(torch.float32).view(2, 4)
+    w2 = w2.view(torch.float32).view(2, 2, 1440).copy_(w0)
+    got = (*X.xattn_decode(qd, cache, td, ld, o=o, lse=lse, weights=w2, workspace=ws), w2)
+    assert all(torch.equal(bits(a), bits(b)) for a, b in zip(want, got))
+    assert bool((buffer[sum(parts):] == 0).all())
+    with pytest.raises(X.XAttnError, match="share memory"):
+        X.xattn_decode(qd, cache, td, ld, o=o, weights=w2, workspace=buffer[at[2]:])

@@ -1,11 +1,14 @@
 """Handles of the serving calls and the numbers and tensors that go to C as they are,
 on the CPU: what would reach a kernel as something else than was given is refused."""
+import ctypes
+
 import pytest
 import torch
 
 import paper_2503_16428_amd as X
+from paper_2503_16428_amd import binding as B
 
-from .test_serving_checks import HostCache, bf, expect, i32
+from .test_serving_checks import HostCache, bf, c_cache, expect, i32
 
 
 def test_a_cache_keeps_its_arrays():
@@ -55,3 +58,59 @@ def test_tensors_that_a_call_needs_are_missed():
     w, new = torch.zeros(3, 2, 32), i32(3, 1)
     expect("lens must be given", X.xattn_cache_evict, c, table, None, w, new, 4, 1)
     expect("weights must be given", X.xattn_cache_evict, c, table, i32(3), None, new, 4, 1)
+
+
+# ---- arrays that share memory (addresses that are never used: every call is refused)
+
+POOL = ("k", "v", "k_scale", "v_scale")
+on_the_cpu = pytest.mark.skipif(torch.cuda.is_available(), reason="calls with made-up addresses")
+
+
+def _laid_out(sizes):
+    """An address for each array, more between them than the largest has."""
+    return {name: (i + 1) << 32 for i, name in enumerate(sizes)}
+
+
+def _decode(cache, at, sizes):
+    return X.lib().xattn_decode(at["q"], cache, 2, 4, at["table"], 100, at["lens"], at["o"],
+                                at["lse"], at["weights"], at["workspace"], sizes["workspace"], None)
+
+
+def _evict(cache, at, sizes):
+    return X.lib().xattn_cache_evict(cache, 2, at["table"], 1100, at["lens"], at["weights"], 20, 3,
+                                     at["new_table"], 2, at["kept"], at["new_lens"],
+                                     at["new_weights"], at["workspace"], sizes["workspace"], None)
+
+
+def _cases():
+    """(call, sizes, written): two sequences, 4 / 2 heads, pages of 16, an 8-bit cache of 300."""
+    pool = dict(k=300 * 2 * 16 * 128, v=300 * 2 * 16 * 128, k_scale=300 * 2 * 16,
+                v_scale=300 * 2 * 16)
+    n = ctypes.c_size_t(0)
+    cache = c_cache(pages=300, type=1)
+    assert X.lib().xattn_decode_workspace_size(cache, 2, 4, 100, 1, ctypes.byref(n)) == 0
+    yield _decode, dict(pool, q=2048, table=800, lens=8, o=2048, lse=32, weights=2 * 2 * 1600 * 4,
+                        workspace=n.value), ("o", "lse", "weights", "workspace")
+    assert X.lib().xattn_evict_workspace_size(cache, 2, 1100, ctypes.byref(n)) == 0
+    yield _evict, dict(pool, table=8800, lens=8, weights=2 * 2 * 17600 * 4, new_table=16,
+                       kept=2 * 2 * 20 * 4, new_lens=8, new_weights=2 * 2 * 32 * 4,
+                       workspace=n.value), ("kept", "new_lens", "new_weights", "workspace")
+
+
+@on_the_cpu
+@pytest.mark.parametrize("which", [0, 1])
+def test_written_arrays_share_no_memory(which):
+    """Every written array against every other, at its first and its last 16 bytes."""
+    call, sizes, written = list(_cases())[which]
+    for a in written:
+        for b in sizes:
+            for first in ((True, False) if a != b else ()):
+                at = _laid_out(sizes)
+                # the 16 aligned bytes with b's first or last one
+                at[a] = at[b] if first else at[b] + (sizes[b] - 1) // 16 * 16
+                if (a, b) == ("o", "q") and first:
+                    continue  # in place
+                cache = c_cache(pages=300, type=1, **{n: at[n] for n in sizes if n in POOL})
+                assert call(cache, at, sizes) == B.XATTN_ERR_ARG, (a, b, first)
+                message = X.lib().xattn_last_error().decode()
+                assert "share memory" in message and a in message and b in message
