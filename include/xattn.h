@@ -348,6 +348,7 @@ typedef struct xattn_rotary_plan {
  *        [batch][tokens][heads][128])
  *   pos  int32 [axes][batch][tokens] device, any values
  *   out  bf16, same shape, strided; x itself with x's strides, or no memory of x
+ *        (which may be another slice of the same buffer)
  * Angles are products in fp64, reduced to a turn before they are rounded, so
  * far positions are as exact as near ones; the rotation is fp32, rounded once.
  * XATTN_ERR_ARG for a bad plan, stride, alignment or NULL.

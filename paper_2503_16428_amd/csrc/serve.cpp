@@ -71,6 +71,17 @@ int check_strides(const int64_t* s, const char* name, int batch, int heads, int 
   return XATTN_OK;
 }
 
+// The rotation's output: x itself, or no memory of x. It is decided where both have the
+// same strides (two slices of one projection, say); others are the caller's to keep apart.
+int check_out(const void* x, const Strides& xs, const void* out, const Strides& os, int batch,
+              int heads, int tokens) {
+  if (xs.batch != os.batch || xs.head != os.head || xs.token != os.token || x == out)
+    return XATTN_OK;
+  const long long apart = ((long long)(uintptr_t)out - (long long)(uintptr_t)x) / 2;
+  if (!xattn::vectors_meet(apart, xs, batch, heads, tokens)) return XATTN_OK;
+  return fail(XATTN_ERR_ARG, "out must be x itself or lie apart from it");
+}
+
 constexpr double kTurn = 0.15915494309189533576888;  // 1 / 2 pi
 
 int check_plan(const xattn_rotary_plan* plan, RotaryParams* out) {
@@ -227,7 +238,8 @@ int xattn_rotary(const void* x, const int64_t* x_strides, int batch, int heads, 
       (rc = check_strides(x_strides, "x", batch, heads, tokens, false, &xs)) ||
       (rc = check_strides(out_strides, "out", batch, heads, tokens, true, &os)) ||
       (rc = check_pointer(x, "x", 16)) || (rc = check_pointer(out, "out", 16)) ||
-      (rc = check_pointer(pos, "pos", 4)))
+      (rc = check_pointer(pos, "pos", 4)) ||
+      (rc = check_out(x, xs, out, os, batch, heads, tokens)))
     return rc;
   return launched(launch_rotary(x, xs, batch, heads, tokens, pos, p, plan->interleaved != 0,
                                 inverse != 0, out, os, (hipStream_t)stream),

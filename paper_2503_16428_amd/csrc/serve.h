@@ -31,6 +31,33 @@ struct Strides {
   long long batch, head, token;
 };
 
+// Whether two arrays of vectors with the same sizes and strides have an element in
+// common, the second one's first element `apart` elements behind the first one's. From
+// the smallest stride on each is at least what the smaller ones span, so that at most
+// two multiples of the largest can come as near as the rest reaches, and so on down.
+inline bool vectors_meet(long long apart, const Strides& s, int batch, int heads, int tokens) {
+  long long stride[3] = {s.batch, s.head, s.token}, size[3] = {batch, heads, tokens};
+  for (int i = 0; i < 3; ++i)
+    for (int j = i + 1; j < 3; ++j)
+      if (stride[j] > stride[i]) {
+        const long long a = stride[i], b = size[i];
+        stride[i] = stride[j], size[i] = size[j];
+        stride[j] = a, size[j] = b;
+      }
+  for (int pick = 0; pick < 8; ++pick) {
+    long long rest = apart;
+    bool inside = true;
+    for (int i = 0; i < 3 && inside; ++i) {
+      if (size[i] == 1) continue;
+      long long n = rest / stride[i] - (rest % stride[i] < 0) + (pick >> i & 1);
+      inside = n > -size[i] && n < size[i];
+      rest -= n * stride[i];
+    }
+    if (inside && rest > -kHeadDim && rest < kHeadDim) return true;
+  }
+  return false;
+}
+
 // A plan as the kernels take it (by value): turns per position of each pair, the
 // first pairs behind axes 0 and 1, and how many pairs are rotated.
 struct RotaryParams {

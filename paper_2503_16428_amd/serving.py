@@ -215,6 +215,10 @@ def _extent(t):
 
 
 def _apart(a, b):
+    """Whether two tensors of one shape lie apart, as far as the C call cannot tell: it can where
+    they have the same strides."""
+    if all(n == 1 or x == y for n, x, y in zip(a.shape, a.stride(), b.stride())):
+        return True
     (a0, a1), (b0, b1) = _extent(a), _extent(b)
     return a1 <= b0 or b1 <= a0
 
@@ -248,8 +252,7 @@ def xattn_rotary(x, pos, rotary: Rotary, inverse=False, out=None, stream=None):
     else:
         _, _, _, os = _vectors(out, "out", x)
         at = _here(x, (out, pos), ("x", "out", "pos"), (pos,))
-        if not (out.data_ptr() == x.data_ptr() and out.stride() == x.stride()) \
-                and not _apart(out, x):
+        if not _apart(out, x):
             _fail("out must be x itself or lie apart from it")
     _check(lib().xattn_rotary(x.data_ptr(), xs, b, h, n, HEAD_DIM, pos.data_ptr(), rotary._ref,
                               1 if inverse else 0, out.data_ptr(), os, _handle(stream, at)))

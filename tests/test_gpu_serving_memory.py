@@ -46,3 +46,23 @@ def test_outputs_may_lie_side_by_side():
     assert bool((buffer[sum(parts):] == 0).all())
     with pytest.raises(X.XAttnError, match="share memory"):
         X.xattn_decode(qd, cache, td, ld, o=o, weights=w2, workspace=buffer[at[2]:])
+
+
+def test_rotary_into_another_slice_of_the_buffer():
+    """The heads of a projection's output to those beside them, which are not over them; in
+    place whatever the strides of dimensions of size 1 say."""
+    plan = X.Rotary([64], X.rotary_freqs([64]))
+    buffer = torch.randn((2, 9, 12, 128), device="cuda").bfloat16()
+    x, out, over = (buffer[:, :, a:a + 4].transpose(1, 2) for a in (0, 4, 2))
+    pos = torch.arange(18, dtype=torch.int32, device="cuda").view(1, 2, 9)
+    want, before = X.xattn_rotary(x, pos, plan), buffer.clone()
+    assert X.xattn_rotary(x, pos, plan, out=out) is out
+    assert torch.equal(bits(out), bits(want))
+    assert torch.equal(bits(buffer[:, :, :4]), bits(before[:, :, :4]))
+    assert torch.equal(bits(buffer[:, :, 8:]), bits(before[:, :, 8:]))
+    with pytest.raises(X.XAttnError, match="apart"):
+        X.xattn_rotary(x, pos, plan, out=over)
+    one = x[:1]  # another batch stride, of one sequence
+    same = one.as_strided(one.shape, (12345 * 8, *one.stride()[1:]))
+    X.xattn_rotary(one, pos[:, :1].contiguous(), plan, out=same)
+    assert torch.equal(bits(one), bits(want[:1]))

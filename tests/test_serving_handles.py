@@ -114,3 +114,14 @@ def test_written_arrays_share_no_memory(which):
                 assert call(cache, at, sizes) == B.XATTN_ERR_ARG, (a, b, first)
                 message = X.lib().xattn_last_error().decode()
                 assert "share memory" in message and a in message and b in message
+
+
+@on_the_cpu
+def test_a_rotation_over_its_input_is_refused():
+    """Slices of 4 heads of a projection's 12, in bytes from the first one."""
+    s = (ctypes.c_int64 * 3)(9 * 12 * 128, 128, 12 * 128)
+    plan = X.Rotary([64], X.rotary_freqs([64]))
+    for heads in (-3, -1, 1, 2, 3, 12, -12, 11 * 9):
+        rc = X.lib().xattn_rotary(1 << 32, s, 2, 4, 9, 128, 1 << 20, plan._ref, 0,
+                                  (1 << 32) + heads * 256, s, None)
+        assert rc == B.XATTN_ERR_ARG and b"apart" in X.lib().xattn_last_error(), heads
