@@ -240,9 +240,14 @@ def _handle(stream, at):
 
 
 def xattn_rotary(x, pos, rotary: Rotary, inverse=False, out=None, stream=None):
-    """x rotated by its positions (back with inverse, which is also the gradient). pos int32
-    [axes, batch, tokens] ([axes, tokens] for 3-D x). out: contiguous if not given; may be x."""
+    """x rotated by its positions (back with inverse, which is also the gradient: nothing is
+    recorded for it, and an x that requires one is refused while gradients are recorded). pos int32
+    [axes, batch, tokens] ([axes, tokens] for 3-D x). out: contiguous if not given; may be x, or
+    another slice of its buffer."""
     b, h, n, xs = _vectors(x, "x")
+    if x.requires_grad and torch.is_grad_enabled():
+        _fail("x requires a gradient, which the call does not record: call it under torch.no_grad() "
+              "(in an autograd function the backward is the call with inverse)")
     _positions(pos, rotary, b, n, x.dim())
     if out is None:
         at = _here(x, (pos,), ("x", "pos"), (pos,))

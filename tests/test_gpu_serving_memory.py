@@ -9,7 +9,8 @@ if not torch.cuda.is_available():
 
 import paper_2503_16428_amd as X  # noqa: E402
 
-from .test_gpu_serving import bits, decode_case, ints, on_gpu  # noqa: E402
+from . import serving_oracle as R  # noqa: E402
+from .test_gpu_serving import bits, decode_case, ints, on_gpu, within  # noqa: E402
 
 
 @pytest.mark.parametrize("hq,hkv,columns", [(4, 2, 4), (4, 2, 80), (40, 1, 4), (40, 1, 80)])
@@ -66,3 +67,29 @@ def test_rotary_into_another_slice_of_the_buffer():
     same = one.as_strided(one.shape, (12345 * 8, *one.stride()[1:]))
     X.xattn_rotary(one, pos[:, :1].contiguous(), plan, out=same)
     assert torch.equal(bits(one), bits(want[:1]))
+
+
+@pytest.mark.parametrize("inverse", [False, True])
+def test_rotary_in_an_autograd_function(inverse):
+    """As a program that wants gradients has it: forward and backward are the two calls."""
+    plan = X.Rotary([30, 20], X.rotary_freqs([30, 20]), True)
+
+    class Turn(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, pos):
+            ctx.save_for_backward(pos)
+            return X.xattn_rotary(x, pos, plan, inverse=inverse)
+
+        @staticmethod
+        def backward(ctx, g):
+            return X.xattn_rotary(g.contiguous(), ctx.saved_tensors[0], plan,
+                                  inverse=not inverse), None
+
+    g = torch.Generator().manual_seed(570)
+    x = torch.randn((2, 3, 5, 128), generator=g).bfloat16()
+    to = torch.randn((2, 3, 5, 128), generator=g).bfloat16()
+    pos = torch.randint(0, 5000, (2, 2, 5), generator=g, dtype=torch.int32)
+    xd = x.cuda().requires_grad_()
+    Turn.apply(xd, pos.cuda()).backward(to.cuda())
+    want, off = R.rotate(to, pos, [30, 20], list(X.rotary_freqs([30, 20])), True, not inverse)
+    within(xd.grad, want, R.bf16_bound(want, off))

@@ -125,3 +125,13 @@ def test_a_rotation_over_its_input_is_refused():
         rc = X.lib().xattn_rotary(1 << 32, s, 2, 4, 9, 128, 1 << 20, plan._ref, 0,
                                   (1 << 32) + heads * 256, s, None)
         assert rc == B.XATTN_ERR_ARG and b"apart" in X.lib().xattn_last_error(), heads
+
+
+def test_a_rotation_does_not_lose_a_gradient_in_silence():
+    plan, pos = X.Rotary([64], X.rotary_freqs([64])), i32(1, 2, 5)
+    x = bf(2, 3, 5, 128).requires_grad_()
+    expect("requires a gradient", X.xattn_rotary, x, pos, plan)
+    expect("requires a gradient", X.xattn_rotary, x * 2, pos, plan, out=bf(2, 3, 5, 128))
+    with torch.no_grad():
+        expect("device tensor", X.xattn_rotary, x, pos, plan)
+    expect("device tensor", X.xattn_rotary, x.detach(), pos, plan)
