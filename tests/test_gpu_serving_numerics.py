@@ -14,7 +14,7 @@ import paper_2503_16428_amd as X  # noqa: E402
 
 from .serving_numerics import (cancelling, in_two_parts, rotated_in_8_bits,  # noqa: E402
                                rotated_in_fp32)
-from .test_gpu_serving import bits, check_decode, decode_case, ints, within  # noqa: E402
+from .test_gpu_serving import bits, check_decode, decode_case, gen, ints, within  # noqa: E402
 
 
 @pytest.mark.parametrize("e4m3", [False, True])
@@ -72,3 +72,28 @@ def test_keys_that_go_to_8_bits_are_turned_in_64(pairs, interleaved):
     byte = cache.k_scale.cpu()[order].transpose(0, 1).reshape(hkv, -1)[:, :tokens]
     assert torch.equal(byte, scale[0])
     assert ((got == bits(least)[0]) | (got == bits(most)[0])).all()
+
+
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("power", [88, -99])
+def test_values_at_the_ends_of_the_supported_range(power, e4m3, wide):
+    """All values near 2^power, every weight alike in one sequence, late large products, which pass
+    the first ones by up to 2^8 before they are followed, in the other."""
+    lens = [700, 700]
+    q, k, v, s, table = decode_case(2, 4, 2, 64, lens, e4m3, wide=wide)
+    sign = torch.where(torch.rand(v.shape, generator=gen(580)) < 0.5, -1.0, 1.0)
+    if e4m3:  # 1 .. 2 times 2^power, the values 256 .. 512 times 2^(power - 8)
+        v = (sign * 256 * (1 + 0.75 * torch.rand(v.shape, generator=gen(581)))).to(v.dtype)
+        s = (s[0], torch.full_like(s[1], 127 + power - 8))
+    else:
+        v = (sign * (1 + torch.rand(v.shape, generator=gen(581)) * 0.9)).bfloat16()
+        v = (v.double() * 2.0 ** power).bfloat16()
+    k[table[0].long()] = k[table[0, 0].long(), :, :1].clone()
+    if e4m3:
+        s[0][table[0].long()] = s[0][table[0, 0].long(), :, :1].clone()
+    q[1] = q[1].abs()
+    for i in range(11):  # page after page a little larger
+        k[table[1, i].long()] = (k[table[1, i].long()].float().abs() * (0.05 + 0.04 * i)).to(k.dtype)
+    o, _, _ = check_decode(q, k, v, s, table, lens)
+    assert torch.isfinite(o.float()).all() and (o.float().abs() > 0).any()
