@@ -349,8 +349,9 @@ typedef struct xattn_rotary_plan {
  *   pos  int32 [axes][batch][tokens] device, any values
  *   out  bf16, same shape, strided; x itself with x's strides, or no memory of x
  *        (which may be another slice of the same buffer)
- * Angles are products in fp64, reduced to a turn before they are rounded, so
- * far positions are as exact as near ones; the rotation is fp32, rounded once.
+ * Angles are products in fp64 (off by 2^-52 of themselves), reduced to a turn before
+ * they are rounded, so far positions are as exact as near ones; sine and cosine are
+ * good to 2.2e-7, the rotation is fp32, rounded once.
  * XATTN_ERR_ARG for a bad plan, stride, alignment or NULL.
  */
 int xattn_rotary(const void *x, const int64_t *x_strides, int batch, int heads, int tokens,
@@ -392,8 +393,9 @@ typedef struct xattn_cache {
  * bf16: a rotated key is rounded once, all else copied. e4m3: the scale is the
  * least power of two (at least 2^-126) that brings the vector's largest finite
  * magnitude to at most 448 (1 for a vector of zeros); a key that is rotated
- * takes the largest length of a pair instead, which bounds it whatever the angle
- * (a pair of which one value is not finite counts with the other). Values are
+ * takes the largest length of a pair instead, its square summed in fp32, which bounds
+ * it whatever the angle (a pair of which one value is not finite counts with the
+ * other); it is turned in fp64. Values are
  * rounded to nearest even; infinities become +-448, NaN stays NaN.
  * No place may be written twice in a call (a page in two tables' rows, for
  * instance): which of the tokens it then holds is not defined.

@@ -1,5 +1,7 @@
 """What the serving calls hold in 32 bits, seen where it shows: outputs that are
 the small rest of large terms, so that their own rounding to bf16 hides nothing."""
+import math
+
 import pytest
 
 from . import serving_oracle as R
@@ -97,3 +99,24 @@ def test_values_at_the_ends_of_the_supported_range(power, e4m3, wide):
         k[table[1, i].long()] = (k[table[1, i].long()].float().abs() * (0.05 + 0.04 * i)).to(k.dtype)
     o, _, _ = check_decode(q, k, v, s, table, lens)
     assert torch.isfinite(o.float()).all() and (o.float().abs() > 0).any()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("at", [1, 1000003])
+def test_sine_and_cosine_in_32_bits(at, interleaved):
+    """Angles that turn a pair's first value to next to nothing: what is left is their error."""
+    g = torch.Generator().manual_seed(590)
+    for _ in range(8):
+        first, second = (1 + torch.rand((2, 64), generator=g)).bfloat16()
+        x = torch.stack([first, second], 1).flatten() if interleaved else torch.cat([first, second])
+        turns = torch.randint(0, 4, (64,), generator=g).double() if at > 1 else torch.zeros(64)
+        freq = ((torch.atan2(first.double(), second.double()) + 2 * math.pi * turns) / at).tolist()
+        x, pos = x.view(1, 1, 1, 128), torch.full((1, 1, 1), at, dtype=torch.int32)
+        out = X.xattn_rotary(x.cuda(), pos.cuda(), X.Rotary([64], freq, interleaved))
+        want, _ = R.rotate(x, pos, [64], freq, interleaved)
+        # the hardware's 1.26e-7, the turn's rounding pi 2^-25, two products and their
+        # difference, half a step of 2^-23 each; angles in 64 bits 2^-51 of up to 8 pi
+        both = first.double() + second.double()
+        both = torch.stack([both, both], 1).flatten() if interleaved else torch.cat([both, both])
+        off = both * (1.26e-7 + math.pi * 2.0 ** -25 + 3 * 2.0 ** -24 + 8 * math.pi * 2.0 ** -51)
+        within(out, want, R.bf16_bound(want, off.view(want.shape)))
