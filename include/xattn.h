@@ -431,7 +431,11 @@ int xattn_cache_append(const void *k, const int64_t *k_strides, const void *v,
  *   workspace  at least xattn_decode_workspace_size() bytes (`weights`: whether
  *            the call has them; 0 for small calls, then it may be NULL), 16-byte
  *            aligned; its contents on entry are ignored. Calls that may run at the
- *            same time need one each.
+ *            same time need one each. Its size follows the table's width, not the
+ *            lengths, which only the device knows: up to 1536 * 520 bytes times the
+ *            query heads of a key head (32 at most) and, with weights, another
+ *            batch * hq * (4 * table_pages * page + 8), all in multiples of 256.
+ *            (64 sequences of 32 heads in a table of 131,072 tokens: 1 GiB.)
  * QK^T and PV run on the bf16 matrix cores with fp32 accumulation (e4m3 values
  * are exact in bf16); the softmax is fp32, and P goes into PV as the sum of three
  * bf16 values, within 2^-29 of it. The output is rounded once.
@@ -453,7 +457,10 @@ int xattn_decode(const void *q, const xattn_cache *cache, int batch, int hq,
  * be shared with other sequences; free them afterwards.
  *   table, lens  the sequences before: int32 [batch][table_pages], [batch];
  *                lens clamped to 0 .. table_pages * page
- *   weights      fp32 [batch][hkv][table_pages * page] (e.g. from xattn_decode)
+ *   weights      fp32 [batch][hkv][table_pages * page], e.g. from xattn_decode. A
+ *                prompt has none of its own: its last queries give it some, each a
+ *                row of xattn_decode with the sequence's pages, its own length and
+ *                its own weights, which are then summed
  *   new_table    int32 [batch][new_pages]: distinct pages, none of them in
  *                `table`; new_pages * page >= budget
  *   kept         int32 [batch][hkv][budget] (output): the tokens kept, ascending,
@@ -462,7 +469,8 @@ int xattn_decode(const void *q, const xattn_cache *cache, int batch, int hq,
  *   new_weights  fp32 [batch][hkv][new_pages * page] (output): the kept tokens'
  *                weights, 0 behind them
  *   workspace    as for xattn_decode, xattn_evict_workspace_size() bytes (0 for
- *                rows of up to 16384 tokens, then it may be NULL)
+ *                tables of up to 16384 tokens, then it may be NULL; else 49,160 for
+ *                every 8192 tokens of the table's width and key head)
  * The weights are 16-byte aligned. 1 <= budget, 0 <= recent <= budget. Page rows
  * behind the kept tokens are left as they were. A token without a page takes its
  * place among the kept ones like any other, by its weight, and there is nothing to

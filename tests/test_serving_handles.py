@@ -135,3 +135,19 @@ def test_a_rotation_does_not_lose_a_gradient_in_silence():
     with torch.no_grad():
         expect("device tensor", X.xattn_rotary, x, pos, plan)
     expect("device tensor", X.xattn_rotary, x.detach(), pos, plan)
+
+
+@pytest.mark.parametrize("batch,hq,hkv,page,pages", [(1, 4, 2, 16, 100), (64, 32, 8, 64, 2048),
+                                                     (3, 80, 2, 16, 70), (5, 17, 1, 256, 33)])
+def test_workspaces_are_as_large_as_the_header_says(batch, hq, hkv, page, pages):
+    c = c_cache(hkv=hkv, page=page)
+    n = ctypes.c_size_t(0)
+    group = min(hq // hkv, 32)
+    parts = 1536 * 520 * group
+    for weights in (0, 1):
+        assert X.lib().xattn_decode_workspace_size(c, batch, hq, pages, weights, ctypes.byref(n)) == 0
+        most = parts + weights * batch * hq * (4 * pages * page + 8)
+        assert most <= n.value < most + 4 * 256
+    assert X.lib().xattn_evict_workspace_size(c, batch, pages, ctypes.byref(n)) == 0
+    chunks = -(-pages * page // 8192) * batch * hkv if pages * page > 16384 else 0
+    assert 49160 * chunks <= n.value <= 49160 * chunks + (batch * hkv * 8 + 512 if chunks else 0)
