@@ -710,9 +710,6 @@ __global__ __launch_bounds__(kJoin) void decode_join(DecodeParams p, int chunks,
     add_weights(p, (i - heads) % chunks, (i - heads) / chunks, weights);
 }
 
-
-size_t align256(size_t x) { return (x + 255) / 256 * 256; }
-
 struct Scratch {
   size_t part, ml, stat, z, bytes;
 };

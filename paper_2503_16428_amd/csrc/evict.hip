@@ -433,8 +433,6 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move(CacheParams c,
   }
 }
 
-size_t align256(size_t x) { return (x + 255) / 256 * 256; }
-
 int chunks_of(const CacheParams& c) { return (c.capacity() + kChunk - 1) / kChunk; }
 
 struct Scratch {
@@ -473,12 +471,12 @@ hipError_t launch_evict(const CacheParams& c, bool e4m3, int batch, const int32_
                         (ChunkCounts*)(at + s.counts), (RowDigit*)(at + s.digits)};
   // one launch where one workgroup has the row (before passes could be saved: 2000
   // tokens of 8 heads 22.6 -> 15.0 us, 4 x 8000 40.0 -> 30.1, 4 x 16,000 45.1 -> 41.8)
-  void (*const one[])(EvictParams) = {c.capacity() <= kChunk ? evict_select<kSteps>
-                                                             : evict_select<2 * kSteps>};
+  void (*const one)(EvictParams) = c.capacity() <= kChunk ? evict_select<kSteps>
+                                                          : evict_select<2 * kSteps>;
   void (*const three[])(EvictParams) = {evict_count, evict_collect, evict_emit};
   hipError_t e;
   for (int i = 0; i < (single ? 1 : 3); ++i) {
-    hipLaunchKernelGGL(single ? one[i] : three[i], dim3((unsigned)(rows * chunks)),
+    hipLaunchKernelGGL(single ? one : three[i], dim3((unsigned)(rows * chunks)),
                        dim3(kSelThreads), 0, st, p);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }

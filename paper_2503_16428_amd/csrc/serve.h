@@ -26,6 +26,9 @@ __host__ __device__ inline int page_column(long long t, int shift, int table_pag
   return t < 0 || (t >> shift) >= table_pages ? -1 : (int)(t >> shift);
 }
 
+// Parts of a workspace begin at multiples of 256 bytes.
+inline size_t align256(size_t x) { return (x + 255) / 256 * 256; }
+
 // One array of vectors, [batch][heads][tokens] with strides in elements.
 struct Strides {
   long long batch, head, token;
