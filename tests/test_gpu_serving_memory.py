@@ -93,3 +93,53 @@ def test_rotary_in_an_autograd_function(inverse):
     Turn.apply(xd, pos.cuda()).backward(to.cuda())
     want, off = R.rotate(to, pos, [30, 20], list(X.rotary_freqs([30, 20])), True, not inverse)
     within(xd.grad, want, R.bf16_bound(want, off))
+
+
+def test_graphs_of_long_evictions():
+    """The eviction of three launches, captured twice on one workspace, replayed on new lengths
+    and weights with eager calls on the same workspace between."""
+    batch, hkv, page, columns, budget = 2, 2, 64, 300, 700
+    pages = batch * (columns + 12)
+    g = torch.Generator().manual_seed(620)
+    k, v = (torch.randn((pages, hkv, page, 128), generator=g).bfloat16() for _ in "kv")
+    order = torch.randperm(pages, generator=g).int()
+    table = order[:batch * columns].view(batch, columns).contiguous().cuda()
+    new_table = order[batch * columns:].view(batch, 12).contiguous().cuda()
+    ws = torch.empty(X.evict_workspace_size(on_gpu(k, v, ()), batch, columns), dtype=torch.uint8,
+                     device="cuda")
+
+    def inputs(i):
+        h = torch.Generator().manual_seed(630 + i)
+        w = torch.rand((batch, hkv, columns * page), generator=h)
+        return ints([19000 - 700 * i, [8193, 600, 17000, 0][i]]), (w * 4).floor().cuda()
+
+    def step(cache, lens, w):
+        return X.xattn_cache_evict(cache, table, lens, w, new_table, budget, 40, workspace=ws)
+
+    graphs = []
+    for _ in range(2):
+        cache, (lens, w) = on_gpu(k, v, ()), inputs(0)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            step(on_gpu(k, v, ()), lens, w)
+        torch.cuda.current_stream().wait_stream(side)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = step(cache, lens, w)
+        torch.cuda.synchronize()
+        graphs.append((graph, cache, lens, w, out))
+    eager = on_gpu(k, v, ())
+    for i in (1, 2, 3, 0):
+        new_lens, new_w = inputs(i)
+        want = [t.clone() for t in step(eager, new_lens, new_w)]
+        for graph, cache, lens, w, out in graphs:
+            lens.copy_(new_lens)
+            w.copy_(new_w)
+            graph.replay()
+        torch.cuda.synchronize()
+        for graph, cache, lens, w, out in graphs:
+            assert all(torch.equal(bits(a), bits(b)) for a, b in zip(out, want)), i
+            assert torch.equal(bits(cache.k), bits(eager.k)), i
+            assert torch.equal(bits(cache.v), bits(eager.v)), i
