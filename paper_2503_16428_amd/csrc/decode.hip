@@ -24,10 +24,10 @@
 // its last row), and decode_join adds them in order.
 //
 // Bound by HBM: with tiles filled up to 16 heads and P in three parts 32 flops a byte
-// of bf16 keys and values, which keeps the matrix cores busy for 6 % of the time
+// of bf16 keys and values, which keeps the matrix cores busy for 8 to 9 % of the time
 // that the loads take. 64 sequences of up to 8000 tokens, 32 / 8 heads, 1.08 GB:
-// 170 us in decode_kernel (6.3 TB/s; a kernel that only loads does 6.2 to 7.0), 5.6
-// in decode_join; one of 128K 81 + 5; e4m3, 16 of up to 20,011, 28 / 4 heads, with
+// 170 us in decode_kernel (6.3 TB/s; a kernel that only loads does 6.2 to 7.0), 5.8
+// in decode_join; one of 128K 82 + 5; e4m3, 16 of up to 20,011, 28 / 4 heads, with
 // weights 37 + 9. About 6 us of each are the chain of first loads and the end.
 #include "serve.h"
 
@@ -722,18 +722,23 @@ int tile_rows_of(int group) {
 
 // Whether every row is one workgroup's: where rows are short, or not long and either
 // many or e4m3 (half the bytes a key). Then there are no parts and no join, and a
-// workspace only for weights. In us, shares and join / whole rows, 32 / 8 heads unless
-// noted, of up to as many keys as the table holds:
-//    512 keys  1 sequence 10.2 / 7.8, e4m3 9.7 / 7.0; 64 24.3 / 17.7, 18.2 / 11.7;
-//              256 71.5 / 55.5, 43.9 / 29.1
-//    640 keys  1 sequence 11.4 / 9.1, 8 12.4 / 10.0, 1 of 4 / 1 heads 10.2 / 9.6
-//    768 keys  1 sequence 10.6 / 10.3, 8 12.3 / 11.5, 1 of 4 / 1 heads 10.0 / 10.9
-//    896 keys  1 sequence 11.7 / 11.5, 8 12.4 / 13.0, 1 of 4 / 1 heads 9.9 / 12.2
-//   1024 keys  1 sequence 10.4 / 12.3, e4m3 9.8 / 9.3; 8 12.3 / 14.4, 11.7 / 10.7;
-//              64 31.8 / 29.6, 23.0 / 18.0; 256 114 / 99, 69 / 53; 64 of 40 / 2 heads
-//              23.5 / 15.7, 20.4 / 14.0; 32 of 24 / 24 heads 41.3 / 43.0, 27.5 / 25.3
-//   2048 keys  1 sequence 10.9 / 22.8, e4m3 10.3 / 17.8; 64 53.4 / 54.1, 34.6 / 30.1;
-//              32 of 24 / 24 heads 80.6 / 92.9, 43.9 / 46.0
+// workspace only for weights. In us a call among others, the launch of the join among
+// them, shares and join / whole rows, 32 / 8 heads unless noted, of up to as many keys as
+// the table holds:
+//    512 keys  1 sequence 11.1 / 9.0, e4m3 10.6 / 8.0; 64 25.0 / 18.0, 19.3 / 12.2;
+//              256 69.0 / 51.2, 47.5 / 32.3
+//    640 keys  1 sequence 11.5 / 9.7, 8 12.7 / 10.8, 1 of 4 / 1 heads 10.9 / 10.1
+//    768 keys  1 sequence 11.1 / 11.1, 8 12.7 / 11.7, 1 of 4 / 1 heads 11.1 / 11.2
+//    896 keys  1 sequence 12.1 / 12.9, e4m3 11.6 / 10.5; 8 13.1 / 13.1, 12.1 / 11.2; 1
+//              of 4 / 1 heads 11.3 / 12.1, 10.6 / 10.0
+//   1024 keys  1 sequence 11.4 / 13.9, e4m3 10.6 / 10.7; 8 13.4 / 14.4, 12.5 / 11.8;
+//              64 33.6 / 30.3, 23.1 / 17.6; 256 112.5 / 98.2, 73.7 / 55.4; 64 of 40 / 2
+//              heads 23.9 / 16.2, 21.2 / 17.0; 32 of 24 / 24 heads 44.0 / 44.5, 28.4 / 25.8
+//   2048 keys  1 sequence 11.3 / 23.8, e4m3 10.5 / 18.6; 64 58.4 / 57.1, 37.0 / 30.5;
+//              32 of 24 / 24 heads 73.5 / 85.4, 46.4 / 48.0
+// The kernels alone, one sequence of 4 / 1 heads, shares + join / whole rows: 512 keys
+// 5.9 + 3.7 / 7.6, 640 5.9 + 3.6 / 8.6, 768 6.0 + 3.6 / 9.7, 896 5.9 + 3.4 / 10.7: the
+// second launch's host time makes up for the longer kernel up to 768.
 bool whole_rows(const CacheParams& c, bool e4m3, int rows) {
   return c.capacity() <= 768 || (c.capacity() <= 1024 && (e4m3 || rows >= 128));
 }

@@ -11,9 +11,11 @@
 // loads the next head's before it turns this one.
 //
 // Bound by HBM, every vector read and written once: 32K tokens of 32 heads 102 us
-// (537 MB, 5.3 TB/s; a copy of that size 5.1), 115,200 of 24 heads 251 us (1.42 GB,
-// 5.7 TB/s), append of 48,542 tokens of 8 heads in e4m3 55 us (5.4 TB/s); one token
-// of 64 sequences 4 us, a chain of loads.
+// (537 MB, 5.3 TB/s; a 1 GB copy 5.15), 115,200 of 24 heads 249 us (1.42 GB, 5.7
+// TB/s). Append of 60,000 tokens of 8 heads in bf16 90 us, rotated or not (5.5 TB/s),
+// in e4m3 64 (5.8); one token of 64 sequences 4 us, a chain of loads. Keys that go to
+// e4m3 rotated are bound by their fp64 sines the more, the fewer heads share them: 8
+// heads 79 us (4.7 TB/s), two heads 3.0 TB/s, one head of 200,000 tokens 61 us (2.5).
 #include <type_traits>
 
 #include "serve.h"

@@ -81,9 +81,9 @@ struct CacheParams {
 // workgroup often begins a new one, which the others of its CU then make up for. All
 // of them have to be resident, or the equal shares take a second turn: of the kernel
 // for two tiles of heads (groups of more than 16) a CU holds two. In us, two / three a
-// CU, 8 key heads, groups of 4: one sequence of 128K 88 / 92, 4 of 32K 88 / 91, 48 of
-// up to 8000 133 / 138, in 8 bits 72 / 78; 64 of up to 8000 183 / 177, 100 / 95, of up
-// to 2000 63 / 59, 44 / 39; 64 of 2048, a row each, 88 / 96. Two tiles: 512 sequences
+// CU, 8 key heads, groups of 4: one sequence of 128K 88 / 92, 4 of 32K 87 / 91, 48 of
+// up to 8000 132 / 137, in 8 bits 77 / 82; 64 of up to 8000 178 / 175, 103 / 99, of up
+// to 2000 60 / 59, 40 / 36; 64 of 2048, a row each, 86 / 93. Two tiles: 512 sequences
 // of up to 4000, 32 / 1 heads, 131 / 144, in 8 bits 94 / 108, all of 4000 184 / 214;
 // 1024 of up to 2000 168 / 190; 600 of up to 2500, 20 / 1 heads, 101 / 115. (Any number
 // that is no multiple of the CUs gives some of them more work: 384, 103 us at 128K.)
