@@ -416,9 +416,9 @@ int xattn_cache_append(const void *k, const int64_t *k_strides, const void *v,
  * a key get o = 0 and lse = -inf; keys whose products are -inf have no weight
  * (their values must be finite, as every value with a weight of 0 must). What a
  * page holds behind the last token has no effect, whatever it is.
- * Sums of weights (up to 2^8) and values are divided last, in fp32: values, those in
- * 8 bits times their scales, may be up to 2^89 in magnitude whatever the length
- * (larger ones may give infinities), and below about 2^-100 they lose bits. The
+ * Values (those in 8 bits times their scales) may be of any finite magnitude: the
+ * weights' sum is divided by last, but no sum on the way passes the largest value.
+ * Values below about 2^-64 lose bits (2^-77 in tables of up to 131,072 tokens). The
  * products q . k, before a key's scale is applied, must be finite in fp32.
  * Several new tokens of one sequence are several rows with the same pages and
  * each its own length.

@@ -120,6 +120,9 @@ struct DecodeParams {
   float* lse;    // or NULL
   int batch, hq, group, row_tiles, tile_rows;
   int most_workers;  // or 0: every row is one workgroup's
+  // 1 / (2^8 times the table's tokens), a factor of the weights in the values' product:
+  // no sum of it then passes the largest value
+  float least;
   float* part;   // [2 workers][tile_rows][128] unnormalised outputs
   float* ml;     // [2 workers][tile_rows][2] (maximum in log2, sum)
   float* stat;   // [batch][hq][2] (maximum in log2, sum) of whole rows, or NULL
@@ -180,7 +183,7 @@ __device__ __forceinline__ int sum_of_wave(int x) {
 // Four elements of a finished row: output head `head`, elements d .. d + 3.
 __device__ __forceinline__ void write_row(const DecodeParams& p, long long head, int d, float top,
                                           float sum, f32x4 out) {
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const float inv = sum == 0.f ? 0.f : 1.f / (sum * p.least);
   typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4;
   const bf16x4 r = {(__bf16)(out[0] * inv), (__bf16)(out[1] * inv), (__bf16)(out[2] * inv),
                     (__bf16)(out[3] * inv)};
@@ -440,9 +443,9 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(Decod
       for (int x = 0; x < RT; ++x)
 #pragma unroll
         for (int i = 0; i < TILES; ++i) {
-          if (E4M3)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) zs[x][i][r] *= scale_of(v_scale[i] >> (8 * r) & 255);
+          for (int r = 0; r < 4; ++r)
+            zs[x][i][r] *= E4M3 ? p.least * scale_of(v_scale[i] >> (8 * r) & 255) : p.least;
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
             const Split w = split(zs[x][i][2 * r], zs[x][i][2 * r + 1]);
@@ -777,6 +780,8 @@ hipError_t launch_decode(const void* q, const CacheParams& c, bool e4m3, int bat
   p.group = hq / c.hkv;
   p.tile_rows = tile_rows_of(p.group);
   p.row_tiles = (p.group + p.tile_rows - 1) / p.tile_rows;
+  p.least = 0x1p-8f;  // the largest weight is up to 2^8
+  for (int n = c.capacity(); n > 1; n = (n + 1) / 2) p.least *= 0.5f;
   p.part = (float*)((char*)scratch + s.part);
   p.ml = (float*)((char*)scratch + s.ml);
   p.stat = weights ? (float*)((char*)scratch + s.stat) : nullptr;

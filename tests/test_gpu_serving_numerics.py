@@ -78,19 +78,23 @@ def test_keys_that_go_to_8_bits_are_turned_in_64(pairs, interleaved):
 
 @pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("e4m3", [False, True])
-@pytest.mark.parametrize("power", [88, -99])
+@pytest.mark.parametrize("power", [127, -77])
 def test_values_at_the_ends_of_the_supported_range(power, e4m3, wide):
     """All values near 2^power, every weight alike in one sequence, late large products, which pass
-    the first ones by up to 2^8 before they are followed, in the other."""
+    the first ones by up to 2^8 before they are followed, in the other; and one element the
+    largest there is in every value."""
     lens = [700, 700]
     q, k, v, s, table = decode_case(2, 4, 2, 64, lens, e4m3, wide=wide)
     sign = torch.where(torch.rand(v.shape, generator=gen(580)) < 0.5, -1.0, 1.0)
-    if e4m3:  # 1 .. 2 times 2^power, the values 256 .. 512 times 2^(power - 8)
-        v = (sign * 256 * (1 + 0.75 * torch.rand(v.shape, generator=gen(581)))).to(v.dtype)
+    if e4m3:  # 1 .. 1.75 times 2^power, the values 256 .. 448 times 2^(power - 8)
+        v = sign * 256 * (1 + 0.75 * torch.rand(v.shape, generator=gen(581)))
+        v[..., 7] = 448.0
+        v = v.to(k.dtype)
         s = (s[0], torch.full_like(s[1], 127 + power - 8))
     else:
         v = (sign * (1 + torch.rand(v.shape, generator=gen(581)) * 0.9)).bfloat16()
         v = (v.double() * 2.0 ** power).bfloat16()
+        v[..., 7] = torch.finfo(torch.bfloat16).max * 2.0 ** (power - 127)
     k[table[0].long()] = k[table[0, 0].long(), :, :1].clone()
     if e4m3:
         s[0][table[0].long()] = s[0][table[0, 0].long(), :, :1].clone()
@@ -99,6 +103,8 @@ def test_values_at_the_ends_of_the_supported_range(power, e4m3, wide):
         k[table[1, i].long()] = (k[table[1, i].long()].float().abs() * (0.05 + 0.04 * i)).to(k.dtype)
     o, _, _ = check_decode(q, k, v, s, table, lens)
     assert torch.isfinite(o.float()).all() and (o.float().abs() > 0).any()
+    most = v[0, 0, 0, 7].float() * (2.0 ** (power - 8) if e4m3 else 1)
+    assert torch.equal(o[..., 7].float().cpu(), torch.full((2, 4), float(most.bfloat16())))
 
 
 @pytest.mark.parametrize("interleaved", [False, True])
