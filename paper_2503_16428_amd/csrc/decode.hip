@@ -26,9 +26,9 @@
 // Bound by HBM: with tiles filled up to 16 heads and P in three parts 32 flops a byte
 // of bf16 keys and values, which keeps the matrix cores busy for 8 to 9 % of the time
 // that the loads take. 64 sequences of up to 8000 tokens, 32 / 8 heads, 1.08 GB:
-// 170 us in decode_kernel (6.3 TB/s; a kernel that only loads does 6.2 to 7.0), 5.8
+// 171 us in decode_kernel (6.3 TB/s; a kernel that only loads does 6.2 to 7.0), 5.8
 // in decode_join; one of 128K 82 + 5; e4m3, 16 of up to 20,011, 28 / 4 heads, with
-// weights 37 + 9. About 6 us of each are the chain of first loads and the end.
+// weights 38 + 9. About 6 us of each are the chain of first loads and the end.
 #include "serve.h"
 
 using namespace xattn;
